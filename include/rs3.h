@@ -413,6 +413,118 @@ rs3_status rs3_attend(const void* Qh, const void* Kh, const void* Vh, int32_t n_
                       int32_t H, int32_t d_h, rs3_dtype dt, int32_t n_splits, float* O, void* ws,
                       size_t ws_bytes, void* stream);
 
+/* ---- norm and rotation of queries and keys -----------------------------------
+ * For tensors that a caller projects itself (the operands of rs3_attend and
+ * rs3_block_attend): every head x of a row becomes
+ *   y = x / sqrt(mean_c(x_c^2) + eps) * gain
+ * and then its first d_rot channels are turned in pairs by the factors of the
+ * row's position, both in fp32, rounded to `dt` once.  Pair p of a head takes
+ * column p of the table: channels (2p, 2p+1) with RS3_PAIRS_ADJACENT (as the
+ * layers' tables, see rs3_layer_set_rope) or (p, p + d_rot/2) with
+ * RS3_PAIRS_HALVES; (a, b) becomes (a cos - b sin, a sin + b cos).
+ * n      : rows (tokens), at most 2^24
+ * Q, K   : [n][H][d_h] and [n][H_kv][d_h] in `dt`; row i starts at element
+ *          i * q_stride (k_stride).  H = 0 (or H_kv = 0) leaves that side out
+ *          (its pointers may be NULL); H + H_kv <= 1024.
+ * d_h    : a multiple of 16, at most 256
+ * gain_q, gain_k : fp32 [d_h], shared by the heads, or NULL for 1
+ * eps    : > 0
+ * table  : fp32 [n_pos][d_rot/2][2] of (cos, sin), NULL with d_rot = 0
+ * d_rot  : channels turned: a multiple of 16, 0 <= d_rot <= d_h
+ * pos    : int32 [n], the table row of each token, or NULL for 0 .. n-1 (then
+ *          n <= n_pos).  Rows with a position below 0 or (with a table) at or
+ *          past n_pos are padding: their outputs are left as they are.
+ * Qo, Ko : outputs, row strides qo_stride and ko_stride; may equal Q and K
+ *          with the same stride (in place), else overlap nothing.
+ * Pointers are device pointers; all but pos are 16-byte aligned and row
+ * strides are whole 16-byte units (RS3_E_INVALID otherwise).  Asynchronous on
+ * `stream`, allocates nothing, one launch for both tensors. */
+typedef enum { RS3_PAIRS_ADJACENT = 0, RS3_PAIRS_HALVES = 1 } rs3_pairing;
+rs3_status rs3_qk_norm_rope(int32_t n, const void* Q, int64_t q_stride, int32_t H, const void* K, int64_t k_stride,
+                            int32_t H_kv, int32_t d_h, rs3_dtype dt, const float* gain_q, const float* gain_k,
+                            float eps, const float* table, int32_t n_pos, int32_t d_rot, int32_t pairing,
+                            const int32_t* pos, void* Qo, int64_t qo_stride, void* Ko, int64_t ko_stride,
+                            void* stream);
+
+/* ---- block-sparse attention ---------------------------------------------------
+ * The read-sparse idea on the side of the keys: the keys lie in blocks of
+ * `block` consecutive rows, a query scores every block by its mean key and
+ * attends to the keys of its top_k best blocks only.  Three calls:
+ *   rs3_block_means  : the mean key of every block (or of those that hold the
+ *                      newest keys, as a cache grows);
+ *   rs3_block_select : each query's blocks;
+ *   rs3_block_attend : softmax attention over the keys of those blocks.
+ * The shape and the row layouts are shared by the three:
+ * n_obj   : caches (objects, streams), 1 .. 4096
+ * n_q     : query rows per object (0: nothing is done); n_obj*n_q <= 2^22
+ * n_kv    : key rows per object, at most 2^26 (0: no keys)
+ * H, H_kv : query heads and key heads, H a multiple of H_kv, H <= 256; query
+ *           head h reads key head h / (H / H_kv)
+ * d_h     : 32, 64, 128 or 256
+ * block   : 32, 64, 128 or 256 keys; n_blk = ceil(n_kv / block); the last
+ *           block may be short
+ * top_k   : blocks per query and key head, 1 .. 256, forced ones included
+ * n_first, n_last : the first n_first and the last n_last blocks that a query
+ *           sees are always among its blocks (>= 0, n_first + n_last <= top_k)
+ * dt      : of Q, K, V, O and the mean keys
+ * x_stride, x_obj_stride (elements) for x = q, k, v, o: row i of object o
+ *           starts at o * x_obj_stride + i * x_stride and holds the heads one
+ *           after the other.  A q, k or v object stride of 0 is one tensor
+ *           shared by all objects.  O's rows must not overlap.
+ * n_vis   : device int32 [n_obj][n_q], how many of its object's first keys each
+ *           query sees (values are taken into [0, n_kv]), NULL for all n_kv.
+ *           Causal prompts, caches of different lengths and padded rows (0)
+ *           are said with it.  Keys that a query does not see do not reach its
+ *           row, whatever they hold (in rs3_block_select the mean of a block
+ *           counts whole once its first key is seen: with causal queries take
+ *           n_last >= 1, which keeps the block that a query ends in).
+ * Tensor pointers are device pointers; Q, K, V, O, Kmean and ws are 16-byte
+ * aligned and strides whole 16-byte units.  Every call is asynchronous on
+ * `stream` and allocates nothing; calls that overlap in time (also as graph
+ * replays) need workspaces of their own. */
+typedef struct {
+  int32_t n_obj, n_q, n_kv, H, H_kv, d_h, block, top_k, n_first, n_last;
+  int32_t dt; /* rs3_dtype */
+  int32_t reserved; /* 0 */
+  int64_t q_stride, q_obj_stride, k_stride, k_obj_stride, v_stride, v_obj_stride, o_stride, o_obj_stride;
+} rs3_block_shape;
+
+/* Kmean [n_obj][H_kv][n_blk][d_h]: the mean of the keys of each block, summed
+ * in fp64 and rounded to `dt` once.
+ * kv_len : device int32 [n_obj], the keys that each object has so far (taken
+ *          into [0, n_kv]), NULL for n_kv: the mean of a block is that of its
+ *          keys below kv_len.
+ * n_new  : 0: every block is computed (0 for blocks without a key); > 0: only
+ *          the blocks that hold the object's last n_new keys are written. */
+rs3_status rs3_block_means(const rs3_block_shape* s /*[host]*/, const void* K, const int32_t* kv_len, int32_t n_new,
+                           void* Kmean, void* stream);
+
+/* For query i of object o and key head g the blocks it sees are 0 ..
+ * ceil(v / block) - 1 with v = n_vis[o][i]; their score is
+ *   s_b = sum over the query heads h of g of q_h . Kmean[o][g][b],
+ * ordered as in fp64 (a score that is no number counts as -inf).  Kept are the
+ * forced blocks and, up to top_k in all, those with the largest scores, ties to
+ * the lower block.
+ * idx   : out int32 [n_obj][n_q][H_kv][top_k], ascending, -1 past the count
+ * count : out int32 [n_obj][n_q][H_kv]
+ * ws    : at least rs3_block_select_workspace_size() bytes */
+rs3_status rs3_block_select_workspace_size(const rs3_block_shape* s /*[host]*/, size_t* bytes);
+rs3_status rs3_block_select(const rs3_block_shape* s /*[host]*/, const void* Q, const void* Kmean,
+                            const int32_t* n_vis, int32_t* idx, int32_t* count, void* ws, size_t ws_bytes,
+                            void* stream);
+
+/* O_h = softmax(q_h K^T / sqrt(d_h)) V over the keys below n_vis of the listed
+ * blocks; 0 for a row without any.  idx and count as rs3_block_select writes
+ * them, or the caller's own lists: a count is taken into [0, top_k], and an
+ * entry that is out of range or not above the entry before it takes no part.
+ * Logits of -inf have weight 0.  The bf16 form rounds the weights to bf16 for
+ * the matrix cores; sums are fp32, and O is rounded to `dt` once.
+ * ws : at least rs3_block_attend_workspace_size() bytes */
+rs3_status rs3_block_attend_workspace_size(const rs3_block_shape* s /*[host]*/, size_t* bytes);
+rs3_status rs3_block_attend(const rs3_block_shape* s /*[host]*/, const void* Q, const void* K, const void* V,
+                            const int32_t* idx, const int32_t* count, const int32_t* n_vis, void* O, void* ws,
+                            size_t ws_bytes, void* stream);
+
 /* ---- the L-layer memory-attention stack on the kept queries -----------------
  * Sec. 3.1 ("Sparse memory attention"): the memory module of the VOS models
  * consists of L layers, each with a self-attention and a cross-attention,
@@ -502,7 +614,11 @@ enum {
   RS3_K_STACK_MERGE = 11,  /* stack: split merge of its attentions */
   RS3_K_STACK_MLP = 12,    /* stack: W_vo + LN3 + MLP chunk partials */
   RS3_K_STACK_ROWS = 13,   /* stack: gather / partial sum + LN1 / scatter */
-  RS3_K_COUNT = 14
+  RS3_K_QK_NORM = 14,      /* norm and rotation of queries and keys */
+  RS3_K_BLOCK_MEANS = 15,  /* mean keys of the blocks */
+  RS3_K_BLOCK_SELECT = 16, /* block scores and lists */
+  RS3_K_BLOCK_ATTEND = 17, /* block-sparse attention */
+  RS3_K_COUNT = 18
 };
 rs3_status rs3_profile_enable(int32_t on, int32_t max_launches);
 rs3_status rs3_profile_report(double* total_ms, int64_t* launches, int64_t* dropped);

@@ -18,6 +18,8 @@ Modules:
   post      closure of the decoded masks and the palette argmax (Sec. 3.3)
   stack     the L-layer memory-attention stack on the kept queries (Sec. 3.1,
             "Sparse memory attention"; the layer is a reading, see its doc)
+  block     norm and rotation of queries and keys, and attention over the
+            blocks of keys that each query selects
 
 Parity unpinned: absolute readout and stack values at the workload sizes (the paper
 prints no tensors and its weights are not available); every other function is

@@ -12,5 +12,7 @@ from ._binding import (  # noqa: F401
     select_workspace_size, select_queries,
     readout_workspace_size, readout, readout_noalloc, commit, frame_workspace_size, frame, readout_commit, write_keepset, close_workspace_size, close_masks,
     attend_workspace_size, attend,
+    RS3_PAIRS_ADJACENT, RS3_PAIRS_HALVES, qk_norm_rope, BlockShape, block_shape, block_means,
+    block_select_workspace_size, block_select, block_attend_workspace_size, block_attend,
     KERNEL_NAMES, profile_enable, profile_reset, profile_report, RS3_STREAM_READ_THREADS, stream_read,
 )

@@ -18,6 +18,7 @@ RS3_MAX_MN = 32768
 RS3_TRACK_WORDS = 6
 RS3_BANK_HDR_WORDS = 8
 RS3_NOALLOC_SCRATCH_BYTES = 16 << 20
+RS3_PAIRS_ADJACENT, RS3_PAIRS_HALVES = 0, 1
 
 lib_path = os.path.join(os.path.dirname(os.path.abspath(__file__)), "librs3.so")
 
@@ -46,6 +47,15 @@ class StackWeights(ctypes.Structure):
     """rs3_stack_weights: one layer's host arrays (see rs3.h)."""
     _fields_ = [(n, c_vp) for n in ("ln1_g", "ln1_b", "Wqs", "Wks", "Wvs", "Wos", "ln2_g", "ln2_b", "Wq", "Wk",
                                     "Wv", "Wo", "ln3_g", "ln3_b", "W1", "W2")]
+
+
+class BlockShape(ctypes.Structure):
+    """rs3_block_shape: sizes and row layouts of the block-sparse attention
+    (block_shape() fills in the strides of packed tensors)."""
+    _fields_ = [(n, c_i32) for n in ("n_obj", "n_q", "n_kv", "H", "H_kv", "d_h", "block", "top_k", "n_first",
+                                     "n_last", "dt", "reserved")] + \
+               [(n, c_i64) for n in ("q_stride", "q_obj_stride", "k_stride", "k_obj_stride", "v_stride",
+                                     "v_obj_stride", "o_stride", "o_obj_stride")]
 
 
 class Rs3Error(RuntimeError):
@@ -96,6 +106,14 @@ _SIGS = {
     "rs3_stack_workspace_size": (c_i32, [c_vp, c_i32, c_i32, ctypes.POINTER(c_sz)]),
     "rs3_stack_readout": (c_i32, [c_vp, ctypes.POINTER(Grid), c_vp, c_vp, c_vp, c_vp, c_i32, c_i32, c_vp, c_i32,
                                   c_vp, c_sz, c_vp]),
+    "rs3_qk_norm_rope": (c_i32, [c_i32, c_vp, c_i64, c_i32, c_vp, c_i64, c_i32, c_i32, c_i32, c_vp, c_vp,
+                                 ctypes.c_float, c_vp, c_i32, c_i32, c_i32, c_vp, c_vp, c_i64, c_vp, c_i64, c_vp]),
+    "rs3_block_means": (c_i32, [ctypes.POINTER(BlockShape), c_vp, c_vp, c_i32, c_vp, c_vp]),
+    "rs3_block_select_workspace_size": (c_i32, [ctypes.POINTER(BlockShape), ctypes.POINTER(c_sz)]),
+    "rs3_block_select": (c_i32, [ctypes.POINTER(BlockShape), c_vp, c_vp, c_vp, c_vp, c_vp, c_vp, c_sz, c_vp]),
+    "rs3_block_attend_workspace_size": (c_i32, [ctypes.POINTER(BlockShape), ctypes.POINTER(c_sz)]),
+    "rs3_block_attend": (c_i32, [ctypes.POINTER(BlockShape), c_vp, c_vp, c_vp, c_vp, c_vp, c_vp, c_vp, c_vp, c_sz,
+                                 c_vp]),
     "rs3_profile_enable": (c_i32, [c_i32, c_i32]),
     "rs3_profile_report": (c_i32, [c_vp, c_vp, c_vp]),
     "rs3_profile_reset": (c_i32, []),
@@ -105,7 +123,8 @@ _SIGS = {
 RS3_STREAM_READ_THREADS = 1024 * 256
 
 KERNEL_NAMES = ["energy", "select", "commit", "commit_append", "copy", "qproj", "attn", "combine",
-                "readout_f32", "merge_commit", "stack_gemm", "stack_merge", "stack_mlp", "stack_rows"]
+                "readout_f32", "merge_commit", "stack_gemm", "stack_merge", "stack_mlp", "stack_rows", "qk_norm",
+                "block_means", "block_select", "block_attend"]
 
 _lib = None
 
@@ -382,6 +401,156 @@ def attend(Q, K, V, n_q: int, n_kv: int, H: int, d_h: int, dtype: int, O, ws=Non
     ws_bytes = 0 if ws is None else ws.numel() * ws.element_size()
     _check(lib().rs3_attend(_ptr(Q), _ptr(K), _ptr(V), n_q, n_kv, H, d_h, dtype, n_splits, _ptr(O), _ptr(ws),
                             ws_bytes, _stream(stream)), "rs3_attend")
+
+
+# ---- norm, rotation and block-sparse attention --------------------------------
+def _check_tensor(name: str, t, numel: int, dtype, device):
+    """Refuses a tensor that the kernels would read or write past, or that
+    lies elsewhere than the call's other tensors."""
+    if t.numel() < numel or t.dtype != dtype or t.device != device or not t.is_contiguous():
+        raise ValueError("%s: %s of %s on %s%s, need %d contiguous elements of %s on %s"
+                         % (name, tuple(t.shape), t.dtype, t.device, "" if t.is_contiguous() else " (strided)", numel,
+                            dtype, device))
+
+
+def _check_rows(name: str, t, last: int, dtype, device):
+    """As _check_tensor for a tensor addressed by strides of its own: `last`
+    elements must follow data_ptr() in its storage."""
+    room = t.untyped_storage().nbytes() // t.element_size() - t.storage_offset()
+    if room < last or t.dtype != dtype or t.device != device:
+        raise ValueError("%s: %d elements of %s on %s, need %d of %s on %s"
+                         % (name, room, t.dtype, t.device, last, dtype, device))
+
+
+def _torch_dtype(dt: int):
+    import torch
+    return torch.bfloat16 if dt == RS3_BF16 else torch.float32
+
+
+def _call_device():
+    import torch
+    return torch.device("cuda", torch.cuda.current_device())
+
+
+def qk_norm_rope(n: int, Q, H: int, K, H_kv: int, d_h: int, dtype: int, Qo, Ko, gain_q=None, gain_k=None,
+                 eps: float = 1e-6, table=None, d_rot: int = 0, pairing: int = RS3_PAIRS_ADJACENT, pos=None,
+                 q_stride: Optional[int] = None, k_stride: Optional[int] = None, qo_stride: Optional[int] = None,
+                 ko_stride: Optional[int] = None, stream=None):
+    """RMS norm of each head of Q [n][H][d_h] and K [n][H_kv][d_h] (None with
+    0 heads) and the rotation of its first d_rot channels by table[pos]."""
+    import torch
+    dev, dt, f32 = _call_device(), _torch_dtype(dtype), torch.float32
+    qs, ks = H * d_h if q_stride is None else q_stride, H_kv * d_h if k_stride is None else k_stride
+    qos, kos = H * d_h if qo_stride is None else qo_stride, H_kv * d_h if ko_stride is None else ko_stride
+    if n > 0:
+        for name, t, stride, heads in (("Q", Q, qs, H), ("Qo", Qo, qos, H), ("K", K, ks, H_kv), ("Ko", Ko, kos, H_kv)):
+            if t is not None and heads > 0:
+                _check_rows(name, t, (n - 1) * stride + heads * d_h, dt, dev)
+    for name, t in (("gain_q", gain_q), ("gain_k", gain_k)):
+        if t is not None:
+            _check_tensor(name, t, d_h, f32, dev)
+    n_pos = 0
+    if table is not None:
+        n_pos = table.shape[0]
+        _check_tensor("table", table, n_pos * d_rot, f32, dev)
+    if pos is not None:
+        _check_tensor("pos", pos, n, torch.int32, dev)
+    _check(lib().rs3_qk_norm_rope(n, _ptr(Q), qs, H, _ptr(K), ks, H_kv, d_h, dtype, _ptr(gain_q), _ptr(gain_k), eps,
+                                  _ptr(table), n_pos, d_rot, pairing, _ptr(pos), _ptr(Qo), qos, _ptr(Ko), kos,
+                                  _stream(stream)), "rs3_qk_norm_rope")
+
+
+def block_shape(dtype: int, n_obj: int, n_q: int, n_kv: int, H: int, H_kv: int, d_h: int, block: int, top_k: int,
+                n_first: int = 0, n_last: int = 0, **strides) -> BlockShape:
+    """A BlockShape for packed tensors [n_obj][rows][heads][d_h]; strides
+    (q_stride=, q_obj_stride=, ...) replace the packed ones."""
+    s = BlockShape(n_obj, n_q, n_kv, H, H_kv, d_h, block, top_k, n_first, n_last, dtype, 0)
+    for x, rows, heads in (("q", n_q, H), ("k", n_kv, H_kv), ("v", n_kv, H_kv), ("o", n_q, H)):
+        row = strides.pop(x + "_stride", heads * d_h)
+        setattr(s, x + "_stride", row)
+        setattr(s, x + "_obj_stride", strides.pop(x + "_obj_stride", rows * row))
+    if strides:
+        raise TypeError("block_shape: unknown %s" % ", ".join(strides))
+    return s
+
+
+def _block_rows(s: BlockShape, name: str, t, x: str, rows: int, heads: int, dev):
+    if rows > 0 and s.n_obj > 0:
+        _check_rows(name, t, (s.n_obj - 1) * getattr(s, x + "_obj_stride") + (rows - 1) * getattr(s, x + "_stride") +
+                    heads * s.d_h, _torch_dtype(s.dt), dev)
+
+
+def _block_means_numel(s: BlockShape) -> int:
+    return s.n_obj * s.H_kv * ((s.n_kv + s.block - 1) // s.block if s.block > 0 else 0) * s.d_h
+
+
+def block_means(shape: BlockShape, K, Kmean, kv_len=None, n_new: int = 0, stream=None):
+    """Kmean [n_obj][H_kv][n_blk][d_h]: the mean key of every block of K, or
+    (n_new > 0) of the blocks that hold each object's last n_new keys."""
+    import torch
+    dev = _call_device()
+    _block_rows(shape, "K", K, "k", shape.n_kv, shape.H_kv, dev)
+    _check_tensor("Kmean", Kmean, _block_means_numel(shape), _torch_dtype(shape.dt), dev)
+    if kv_len is not None:
+        _check_tensor("kv_len", kv_len, shape.n_obj, torch.int32, dev)
+    _check(lib().rs3_block_means(ctypes.byref(shape), _ptr(K), _ptr(kv_len), n_new, _ptr(Kmean), _stream(stream)),
+           "rs3_block_means")
+
+
+def block_select_workspace_size(shape: BlockShape) -> int:
+    out = c_sz()
+    _check(lib().rs3_block_select_workspace_size(ctypes.byref(shape), ctypes.byref(out)),
+           "rs3_block_select_workspace_size")
+    return out.value
+
+
+def _check_lists(shape: BlockShape, idx, count, n_vis, dev):
+    import torch
+    rows = shape.n_obj * shape.n_q
+    _check_tensor("idx", idx, rows * shape.H_kv * shape.top_k, torch.int32, dev)
+    _check_tensor("count", count, rows * shape.H_kv, torch.int32, dev)
+    if n_vis is not None:
+        _check_tensor("n_vis", n_vis, rows, torch.int32, dev)
+
+
+def _workspace(ws, dev):
+    if ws is None:
+        return None, 0
+    if ws.device != dev or not ws.is_contiguous():
+        raise ValueError("ws: on %s, need contiguous memory on %s" % (ws.device, dev))
+    return ws.data_ptr(), ws.numel() * ws.element_size()
+
+
+def block_select(shape: BlockShape, Q, Kmean, idx, count, n_vis=None, ws=None, stream=None):
+    """Each query's blocks by the scores of their mean keys: idx int32
+    [n_obj][n_q][H_kv][top_k] ascending (-1 past the count), count int32."""
+    dev = _call_device()
+    _block_rows(shape, "Q", Q, "q", shape.n_q, shape.H, dev)
+    _check_tensor("Kmean", Kmean, _block_means_numel(shape), _torch_dtype(shape.dt), dev)
+    _check_lists(shape, idx, count, n_vis, dev)
+    p, nbytes = _workspace(ws, dev)
+    _check(lib().rs3_block_select(ctypes.byref(shape), _ptr(Q), _ptr(Kmean), _ptr(n_vis), _ptr(idx), _ptr(count), p,
+                                  nbytes, _stream(stream)), "rs3_block_select")
+
+
+def block_attend_workspace_size(shape: BlockShape) -> int:
+    out = c_sz()
+    _check(lib().rs3_block_attend_workspace_size(ctypes.byref(shape), ctypes.byref(out)),
+           "rs3_block_attend_workspace_size")
+    return out.value
+
+
+def block_attend(shape: BlockShape, Q, K, V, idx, count, O, n_vis=None, ws=None, stream=None):
+    """Softmax attention of every query over the keys of its listed blocks."""
+    dev = _call_device()
+    _block_rows(shape, "Q", Q, "q", shape.n_q, shape.H, dev)
+    _block_rows(shape, "K", K, "k", shape.n_kv, shape.H_kv, dev)
+    _block_rows(shape, "V", V, "v", shape.n_kv, shape.H_kv, dev)
+    _block_rows(shape, "O", O, "o", shape.n_q, shape.H, dev)
+    _check_lists(shape, idx, count, n_vis, dev)
+    p, nbytes = _workspace(ws, dev)
+    _check(lib().rs3_block_attend(ctypes.byref(shape), _ptr(Q), _ptr(K), _ptr(V), _ptr(idx), _ptr(count), _ptr(n_vis),
+                                  _ptr(O), p, nbytes, _stream(stream)), "rs3_block_attend")
 
 
 class Stack:

@@ -14,7 +14,7 @@ ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 OBJDIR = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "librs3.so")
-SOURCES = ["host_check.cpp", "select.hip", "commit.hip", "readout.hip", "attn_tile.hip", "readout_f32.hip", "attend.hip", "rope.hip", "keepset.hip", "post.hip", "fused.hip", "stack.hip", "api.hip", "profile.hip"]
+SOURCES = ["host_check.cpp", "select.hip", "commit.hip", "readout.hip", "attn_tile.hip", "readout_f32.hip", "attend.hip", "rope.hip", "keepset.hip", "post.hip", "fused.hip", "stack.hip", "api.hip", "profile.hip", "qk_norm.hip", "block_means.hip", "block_select.hip", "block_attend.hip", "block_api.hip"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 # The attention kernel keeps its MFMA accumulators in arch VGPRs, so the

@@ -1,0 +1,216 @@
+// Host side of the norm and rotation of queries and keys and of the
+// block-sparse attention: validation and launch arguments.
+#include <math.h>
+#include <string.h>
+
+#include "block.h"
+
+using namespace rs3;
+
+namespace {
+
+rs3_status map_err(hipError_t e) {
+  if (e == hipSuccess) return RS3_OK;
+  return e == hipErrorOutOfMemory ? RS3_E_OOM : RS3_E_DEVICE;
+}
+
+bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
+size_t elem(int dt) { return dt == RS3_BF16 ? 2 : 4; }
+
+// A stride of whole 16-byte units, small enough that no row's offset leaves
+// 62 bits.
+bool stride_ok(int64_t s, size_t es) { return s >= 0 && s < (1ll << 36) && s * es % 16 == 0; }
+
+bool shape_ok(const rs3_block_shape* s) {
+  if (!s || (s->dt != RS3_BF16 && s->dt != RS3_F32) || s->reserved != 0) return false;
+  if (s->n_obj < 1 || s->n_obj > 4096 || s->n_q < 0 || (int64_t)s->n_obj * s->n_q > (1 << 22)) return false;
+  if (s->n_kv < 0 || s->n_kv > (1 << 26)) return false;
+  if (s->H < 1 || s->H > 256 || s->H_kv < 1 || s->H % s->H_kv != 0) return false;
+  if (s->d_h != 32 && s->d_h != 64 && s->d_h != 128 && s->d_h != 256) return false;
+  if (s->block != 32 && s->block != 64 && s->block != 128 && s->block != 256) return false;
+  if (s->top_k < 1 || s->top_k > 256 || s->n_first < 0 || s->n_last < 0) return false;
+  return (int64_t)s->n_first + s->n_last <= s->top_k;
+}
+
+// Row layout of a tensor with `heads` heads a row.
+bool rows_ok(const rs3_block_shape* s, int64_t row, int64_t obj, int heads) {
+  const size_t es = elem(s->dt);
+  return stride_ok(row, es) && stride_ok(obj, es) && row >= (int64_t)heads * s->d_h;
+}
+
+bool out_rows_ok(const rs3_block_shape* s) {
+  const int64_t w = (int64_t)s->H * s->d_h;
+  if (!rows_ok(s, s->o_stride, s->o_obj_stride, s->H)) return false;
+  if (s->n_obj == 1 || s->n_q == 0) return true;
+  return s->o_obj_stride >= w && (s->o_obj_stride >= (int64_t)(s->n_q - 1) * s->o_stride + w ||
+                                  s->o_stride >= (int64_t)(s->n_obj - 1) * s->o_obj_stride + w);
+}
+
+int n_blocks(const rs3_block_shape* s) { return (s->n_kv + s->block - 1) / s->block; }
+
+size_t select_ws(const rs3_block_shape* s) {
+  return (size_t)s->n_obj * s->n_q * s->H_kv * n_blocks(s) * sizeof(double);
+}
+
+}  // namespace
+
+extern "C" {
+
+rs3_status rs3_qk_norm_rope(int32_t n, const void* Q, int64_t q_stride, int32_t H, const void* K, int64_t k_stride,
+                            int32_t H_kv, int32_t d_h, rs3_dtype dt, const float* gain_q, const float* gain_k,
+                            float eps, const float* table, int32_t n_pos, int32_t d_rot, int32_t pairing,
+                            const int32_t* pos, void* Qo, int64_t qo_stride, void* Ko, int64_t ko_stride,
+                            void* stream) {
+  if (n < 0 || n > (1 << 24) || (dt != RS3_BF16 && dt != RS3_F32)) return RS3_E_INVALID;
+  if (H < 0 || H_kv < 0 || H > 1024 || H_kv > 1024 - H || d_h < 16 || d_h > 256 || d_h % 16 != 0) return RS3_E_INVALID;
+  if (!(eps > 0.f) || !isfinite(eps)) return RS3_E_INVALID;
+  if (d_rot < 0 || d_rot > d_h || d_rot % 16 != 0 || (d_rot > 0) != (table != nullptr)) return RS3_E_INVALID;
+  if (pairing != RS3_PAIRS_ADJACENT && pairing != RS3_PAIRS_HALVES) return RS3_E_INVALID;
+  if (d_rot > 0 && (n_pos < 1 || (!pos && n > n_pos))) return RS3_E_INVALID;
+  if (!aligned16(table) || !aligned16(gain_q) || !aligned16(gain_k)) return RS3_E_INVALID;
+  QkNormArgs a;
+  memset(&a, 0, sizeof(a));
+  const struct {
+    const void* x;
+    void* y;
+    int64_t xs, ys;
+    int heads;
+    const float* gain;
+  } sides[2] = {{Q, Qo, q_stride, qo_stride, H, gain_q}, {K, Ko, k_stride, ko_stride, H_kv, gain_k}};
+  for (int i = 0; i < 2; ++i) {
+    const auto& s = sides[i];
+    if (s.heads == 0) continue;
+    const size_t es = elem(dt);
+    if (n > 0 && (!s.x || !s.y)) return RS3_E_INVALID;
+    if (!aligned16(s.x) || !aligned16(s.y) || !stride_ok(s.xs, es) || !stride_ok(s.ys, es)) return RS3_E_INVALID;
+    if (s.xs < (int64_t)s.heads * d_h || s.ys < (int64_t)s.heads * d_h) return RS3_E_INVALID;
+    if (s.x == s.y && s.xs != s.ys) return RS3_E_INVALID;
+    a.X[i] = s.x;
+    a.Y[i] = s.y;
+    a.xs[i] = s.xs;
+    a.ys[i] = s.ys;
+    a.heads[i] = s.heads;
+    a.gain[i] = s.gain;
+  }
+  if (n == 0 || H + H_kv == 0) return RS3_OK;
+  a.n = n;
+  a.d_h = d_h;
+  a.d_rot = d_rot;
+  a.halves = pairing == RS3_PAIRS_HALVES;
+  a.n_pos = n_pos;
+  a.eps = eps;
+  a.inv_d = 1.f / (float)d_h;
+  a.table = table;
+  a.pos = pos;
+  return map_err(rs3_launch_qk_norm(a, dt, (hipStream_t)stream));
+}
+
+rs3_status rs3_block_means(const rs3_block_shape* s, const void* K, const int32_t* kv_len, int32_t n_new, void* Kmean,
+                           void* stream) {
+  if (!shape_ok(s) || n_new < 0 || !rows_ok(s, s->k_stride, s->k_obj_stride, s->H_kv)) return RS3_E_INVALID;
+  if (!aligned16(K) || !aligned16(Kmean) || (s->n_kv > 0 && (!K || !Kmean))) return RS3_E_INVALID;
+  if (s->n_kv == 0) return RS3_OK;
+  BlockMeansArgs a;
+  memset(&a, 0, sizeof(a));
+  a.K = K;
+  a.ks = s->k_stride;
+  a.ko = s->k_obj_stride;
+  a.kv_len = kv_len;
+  a.Kmean = Kmean;
+  a.n_kv = s->n_kv;
+  a.H_kv = s->H_kv;
+  a.d_h = s->d_h;
+  a.block = s->block;
+  a.n_blk = n_blocks(s);
+  a.n_new = n_new;
+  return map_err(rs3_launch_block_means(a, s->n_obj, s->dt, (hipStream_t)stream));
+}
+
+rs3_status rs3_block_select_workspace_size(const rs3_block_shape* s, size_t* bytes) {
+  if (!bytes || !shape_ok(s)) return RS3_E_INVALID;
+  *bytes = select_ws(s);
+  return RS3_OK;
+}
+
+rs3_status rs3_block_select(const rs3_block_shape* s, const void* Q, const void* Kmean, const int32_t* n_vis,
+                            int32_t* idx, int32_t* count, void* ws, size_t ws_bytes, void* stream) {
+  if (!shape_ok(s) || !rows_ok(s, s->q_stride, s->q_obj_stride, s->H)) return RS3_E_INVALID;
+  if (!aligned16(Q) || !aligned16(Kmean) || !aligned16(ws)) return RS3_E_INVALID;
+  if (s->n_q == 0) return RS3_OK;
+  if (!Q || !idx || !count || (s->n_kv > 0 && !Kmean)) return RS3_E_INVALID;
+  const size_t need = select_ws(s);
+  if (need > 0 && (!ws || ws_bytes < need)) return RS3_E_INVALID;
+  BlockSelectArgs a;
+  memset(&a, 0, sizeof(a));
+  a.Q = Q;
+  a.qs = s->q_stride;
+  a.qo = s->q_obj_stride;
+  a.Kmean = Kmean;
+  a.n_vis = n_vis;
+  a.idx = idx;
+  a.count = count;
+  a.score = (double*)ws;
+  a.rows = (int64_t)s->n_obj * s->n_q * s->H_kv;
+  a.n_obj = s->n_obj;
+  a.n_q = s->n_q;
+  a.n_kv = s->n_kv;
+  a.H = s->H;
+  a.H_kv = s->H_kv;
+  a.d_h = s->d_h;
+  a.block = s->block;
+  a.n_blk = n_blocks(s);
+  a.top_k = s->top_k;
+  a.n_first = s->n_first;
+  a.n_last = s->n_last;
+  return map_err(rs3_launch_block_select(a, s->dt, (hipStream_t)stream));
+}
+
+rs3_status rs3_block_attend_workspace_size(const rs3_block_shape* s, size_t* bytes) {
+  if (!bytes || !shape_ok(s)) return RS3_E_INVALID;
+  *bytes = 0;
+  return RS3_OK;
+}
+
+rs3_status rs3_block_attend(const rs3_block_shape* s, const void* Q, const void* K, const void* V, const int32_t* idx,
+                            const int32_t* count, const int32_t* n_vis, void* O, void* ws, size_t ws_bytes,
+                            void* stream) {
+  if (!shape_ok(s) || !rows_ok(s, s->q_stride, s->q_obj_stride, s->H) ||
+      !rows_ok(s, s->k_stride, s->k_obj_stride, s->H_kv) || !rows_ok(s, s->v_stride, s->v_obj_stride, s->H_kv) ||
+      !out_rows_ok(s))
+    return RS3_E_INVALID;
+  if (!aligned16(Q) || !aligned16(K) || !aligned16(V) || !aligned16(O) || !aligned16(ws)) return RS3_E_INVALID;
+  if (s->n_q == 0) return RS3_OK;
+  if (!Q || !idx || !count || !O || (s->n_kv > 0 && (!K || !V))) return RS3_E_INVALID;
+  if (O == Q || (s->n_kv > 0 && (O == K || O == V))) return RS3_E_INVALID;
+  BlockAttendArgs a;
+  memset(&a, 0, sizeof(a));
+  a.Q = Q;
+  a.K = K;
+  a.V = V;
+  a.O = O;
+  a.qs = s->q_stride;
+  a.qo = s->q_obj_stride;
+  a.ks = s->k_stride;
+  a.ko = s->k_obj_stride;
+  a.vs = s->v_stride;
+  a.vo = s->v_obj_stride;
+  a.os = s->o_stride;
+  a.oo = s->o_obj_stride;
+  a.idx = idx;
+  a.count = count;
+  a.n_vis = n_vis;
+  a.qscale = (float)(1.4426950408889634 / sqrt((double)s->d_h));
+  a.n_obj = s->n_obj;
+  a.n_q = s->n_q;
+  a.n_kv = s->n_kv;
+  a.H = s->H;
+  a.H_kv = s->H_kv;
+  a.G = s->H / s->H_kv;
+  a.d_h = s->d_h;
+  a.block = s->block;
+  a.n_blk = n_blocks(s);
+  a.top_k = s->top_k;
+  return map_err(rs3_launch_block_attend(a, s->dt, (hipStream_t)stream));
+}
+
+}  // extern "C"

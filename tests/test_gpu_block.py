@@ -1,0 +1,541 @@
+"""Norm and rotation of queries and keys and the block-sparse attention
+against the fp64 oracle.
+
+Tolerances.  A value rounded to the output type is off by at most half a
+step, u = finfo.eps / 2 relative (bf16 2^-8, fp32 2^-24).
+Norm: a sum of d_h squares, a root, a quotient, two products and a rotation in
+fp32 are off by at most (d_h/2 + 16) 2^-24 of the largest magnitude of the
+row's turned pairs.
+Means: summed in fp64, rounded to fp32 and then to the type.
+Select: equal lists (scores are ordered as in fp64).
+Attend: a logit is off by delta = (d_h + 4) 2^-24 sum|q_c k_c|/sqrt(d_h) plus
+2^-22 of it for the scaling and exponential, so a weight by that relative to
+itself; in bf16 each weight is also rounded to bf16 (2^-8), in the numerator
+and in the sum, and partial rows are kept to 2^-11 of their largest value; the
+result is rounded once.  With A = sum_j w_j |v_j| this gives
+  |err| <= (2 delta + 2 u_w + u_p + n 2^-24) A + u |O|.
+"""
+import numpy as np
+import pytest
+
+from oracle import block as B
+from workloads import storage_to_f64, to_storage
+
+pytestmark = pytest.mark.gpu
+torch = pytest.importorskip("torch")
+
+U = {"bf16": 2.0 ** -8, "f32": 2.0 ** -24}
+
+
+def rs3():
+    import paper_2608_22526_amd as p
+    return p
+
+
+def dt_of(dtype):
+    return rs3().RS3_BF16 if dtype == "bf16" else rs3().RS3_F32
+
+
+def dev(a):
+    from paper_2608_22526_amd.session import to_device
+    return to_device(a)
+
+
+def host(t, dtype):
+    from paper_2608_22526_amd.session import to_host
+    return storage_to_f64(to_host(t), dtype)
+
+
+def draw(rng, shape, dtype, scale=1.0):
+    return to_storage((scale * rng.standard_normal(shape, dtype=np.float32)).astype(np.float32), dtype)
+
+
+# ---- norm and rotation ---------------------------------------------------------
+def run_norm(n, H, H_kv, d_h, dtype, d_rot, halves, seed, use_pos=True, gains=True, pad=0, in_place=False, extra=0):
+    p = rs3()
+    rng = np.random.default_rng(seed)
+    n_pos = n + 7
+    table = None
+    if d_rot:
+        ang = rng.uniform(-np.pi, np.pi, (n_pos, d_rot // 2))
+        table = np.stack([np.cos(ang), np.sin(ang)], -1).astype(np.float32)
+    pos = rng.permutation(n_pos)[:n].astype(np.int32) if use_pos else None
+    if pad:
+        bad = rng.choice(n, pad, replace=False)
+        pos[bad] = np.where(np.arange(pad) % 2 == 0, -1 - np.arange(pad), n_pos + np.arange(pad) if d_rot else -5)
+    dt = dt_of(dtype)
+    outs = []
+    tq, tk = [], []
+    sides = []
+    for heads in (H, H_kv):
+        w = heads * d_h + extra
+        x = draw(rng, (n, w), dtype, 3.0)
+        gain = (1 + 0.3 * rng.standard_normal(d_h)).astype(np.float32) if gains else None
+        X = dev(x)
+        Y = X if in_place else torch.full_like(X, 7.0)
+        sides.append((heads, x, gain, X, Y, w))
+    (h0, x0, g0, X0, Y0, w0), (h1, x1, g1, X1, Y1, w1) = sides
+    p.qk_norm_rope(n, X0 if H else None, H, X1 if H_kv else None, H_kv, d_h, dt, Y0 if H else None,
+                   Y1 if H_kv else None, gain_q=None if g0 is None else dev(g0), gain_k=None if g1 is None else dev(g1),
+                   eps=1e-5, table=None if table is None else dev(table), d_rot=d_rot,
+                   pairing=p.RS3_PAIRS_HALVES if halves else p.RS3_PAIRS_ADJACENT,
+                   pos=None if pos is None else dev(pos), q_stride=w0, k_stride=w1, qo_stride=w0, ko_stride=w1)
+    torch.cuda.synchronize()
+    for heads, x, gain, X, Y, w in sides:
+        if heads == 0:
+            continue
+        got = host(Y, dtype)
+        before = storage_to_f64(x, dtype) if in_place else np.full(got.shape, 7.0)
+        xs = storage_to_f64(x, dtype)[:, :heads * d_h].reshape(n, heads, d_h)
+        exp = B.norm_rope(xs, gain, 1e-5, table, pos, halves)
+        out = np.zeros(n, bool) if pos is None else (pos < 0) | ((pos >= n_pos) if d_rot else False)
+        assert np.array_equal(got[out], before[out])               # padding rows
+        assert np.array_equal(got[:, heads * d_h:], before[:, heads * d_h:])   # between the rows
+        g = got[~out][:, :heads * d_h].reshape(-1, heads, d_h)
+        e = exp[~out]
+        tol = U[dtype] * np.abs(e) + (d_h / 2 + 16) * 2.0 ** -24 * 2 * np.abs(e).max(-1, keepdims=True, initial=0)
+        assert (np.abs(g - e) <= tol).all(), np.abs(g - e).max()
+
+
+@pytest.mark.parametrize("n,H,H_kv,d_h,dtype,d_rot,halves", [
+    (1, 1, 1, 16, "bf16", 16, False), (1, 32, 8, 128, "bf16", 128, True), (77, 8, 8, 32, "bf16", 32, False),
+    (130, 6, 2, 64, "bf16", 32, True), (33, 3, 1, 80, "bf16", 80, False), (33, 3, 1, 80, "bf16", 80, True),
+    (50, 5, 5, 96, "bf16", 48, True), (41, 4, 2, 256, "bf16", 256, True), (41, 4, 2, 256, "bf16", 64, False),
+    (1, 2, 1, 16, "f32", 16, True), (65, 4, 4, 64, "f32", 64, False), (29, 2, 2, 80, "f32", 48, True),
+    (29, 3, 1, 128, "f32", 128, True), (19, 2, 1, 256, "f32", 256, True), (19, 2, 1, 240, "f32", 240, False),
+    (64, 0, 8, 64, "bf16", 64, True), (64, 8, 0, 64, "bf16", 0, True), (300, 40, 3, 48, "bf16", 16, True)])
+def test_norm_rope(n, H, H_kv, d_h, dtype, d_rot, halves):
+    run_norm(n, H, H_kv, d_h, dtype, d_rot, halves, seed=n + d_h + d_rot)
+
+
+@pytest.mark.parametrize("kw", [dict(use_pos=False), dict(gains=False), dict(pad=9), dict(in_place=True),
+                                dict(extra=64), dict(in_place=True, pad=5, extra=32)])
+@pytest.mark.parametrize("dtype,halves", [("bf16", True), ("f32", False)])
+def test_norm_rope_options(kw, dtype, halves):
+    run_norm(60, 6, 2, 64, dtype, 64, halves, seed=3, **kw)
+
+
+def test_norm_rope_padding_without_table():
+    run_norm(40, 4, 4, 32, "bf16", 0, False, seed=4, pad=11)
+
+
+# ---- means ---------------------------------------------------------------------
+@pytest.mark.parametrize("n_obj,n_kv,H_kv,d_h,block,dtype", [
+    (1, 1, 1, 32, 32, "bf16"), (3, 100, 2, 64, 32, "bf16"), (2, 515, 3, 128, 64, "bf16"), (2, 700, 1, 256, 256, "bf16"),
+    (2, 129, 2, 64, 128, "f32"), (1, 64, 2, 256, 64, "f32")])
+@pytest.mark.parametrize("ragged", [False, True])
+def test_block_means(n_obj, n_kv, H_kv, d_h, block, dtype, ragged):
+    p = rs3()
+    rng = np.random.default_rng(n_kv + d_h)
+    extra = 32 if ragged else 0
+    K = draw(rng, (n_obj, n_kv, H_kv * d_h + extra), dtype)
+    s = p.block_shape(dt_of(dtype), n_obj, 1, n_kv, H_kv, H_kv, d_h, block, 1, k_stride=H_kv * d_h + extra)
+    kv_len = rng.integers(0, n_kv + 1, n_obj).astype(np.int32) if ragged else None
+    if ragged:
+        kv_len[-1] = n_kv + 5          # taken into [0, n_kv]
+    nb = -(-n_kv // block)
+    M = torch.full((n_obj, H_kv, nb, d_h), 9.0, device="cuda", dtype=dev(K).dtype)
+    p.block_means(s, dev(K), M, kv_len=None if kv_len is None else dev(kv_len))
+    torch.cuda.synchronize()
+    Kf = storage_to_f64(K, dtype)[..., :H_kv * d_h].reshape(n_obj, n_kv, H_kv, d_h)
+    exp = B.block_means(Kf, kv_len if ragged else [n_kv] * n_obj, block)
+    assert (np.abs(host(M, dtype) - exp) <= (U[dtype] + 2.0 ** -23) * np.abs(exp)).all()
+
+
+@pytest.mark.parametrize("n_new", [1, 2, 33, 64, 65, 400, 2 ** 31 - 1])
+def test_block_means_of_new_keys(n_new):
+    """Only the blocks that hold each object's last n_new keys are written."""
+    p = rs3()
+    rng = np.random.default_rng(n_new % 1000)
+    n_obj, n_kv, H_kv, d_h, block = 5, 400, 2, 32, 64
+    K = draw(rng, (n_obj, n_kv, H_kv, d_h), "bf16")
+    kv_len = np.array([400, 0, 1, 64, 129], np.int32)
+    s = p.block_shape(p.RS3_BF16, n_obj, 1, n_kv, H_kv, H_kv, d_h, block, 1)
+    M = torch.full((n_obj, H_kv, 7, d_h), 9.0, device="cuda", dtype=torch.bfloat16)
+    p.block_means(s, dev(K), M, kv_len=dev(kv_len), n_new=n_new)
+    torch.cuda.synchronize()
+    exp = B.block_means(storage_to_f64(K, "bf16"), kv_len, block)
+    got = host(M, "bf16")
+    for o in range(n_obj):
+        b0, b1 = max(0, int(kv_len[o]) - n_new) // block, -(-int(kv_len[o]) // block)
+        assert (np.abs(got[o, :, b0:b1] - exp[o, :, b0:b1]) <= (2.0 ** -8 + 2.0 ** -23) * np.abs(exp[o, :, b0:b1])).all()
+        assert (got[o, :, :b0] == 9).all() and (got[o, :, b1:] == 9).all()
+
+
+# ---- select --------------------------------------------------------------------
+def lengths(rng, n_obj, n_q, n_kv, vis):
+    if vis == "all":
+        return None
+    if vis == "causal":
+        v = np.broadcast_to(np.arange(n_q) + (n_kv - n_q + 1), (n_obj, n_q))
+        return np.ascontiguousarray(v.astype(np.int32))       # may fall below 0
+    v = rng.integers(-2, n_kv + 3, (n_obj, n_q)).astype(np.int32)
+    v.flat[:: 5] = 0
+    return v
+
+
+def run_select(n_obj, n_q, n_kv, H, H_kv, d_h, block, top_k, first, last, vis, dtype, seed, make=None):
+    p = rs3()
+    rng = np.random.default_rng(seed)
+    nb = -(-n_kv // block)
+    Q = draw(rng, (n_obj, n_q, H, d_h), dtype)
+    M = draw(rng, (n_obj, H_kv, nb, d_h), dtype)
+    if make is not None:
+        Q, M = make(rng, Q, M)
+    v = lengths(rng, n_obj, n_q, n_kv, vis)
+    s = p.block_shape(dt_of(dtype), n_obj, n_q, n_kv, H, H_kv, d_h, block, top_k, first, last)
+    idx = torch.full((n_obj, n_q, H_kv, top_k), 77, dtype=torch.int32, device="cuda")
+    count = torch.full((n_obj, n_q, H_kv), 77, dtype=torch.int32, device="cuda")
+    ws = torch.full((max(p.block_select_workspace_size(s), 16),), 0xFF, dtype=torch.uint8, device="cuda")
+    p.block_select(s, dev(Q), dev(M), idx, count, n_vis=None if v is None else dev(v), ws=ws)
+    torch.cuda.synchronize()
+    vis_all = np.full((n_obj, n_q), n_kv) if v is None else v
+    ei, ec = B.block_select(storage_to_f64(Q, dtype), storage_to_f64(M, dtype), vis_all, block, top_k, first, last, n_kv)
+    assert (count.cpu().numpy() != ec).sum() == 0
+    assert (idx.cpu().numpy() != ei).sum() == 0
+
+
+@pytest.mark.parametrize("n_obj,n_q,n_kv,H,H_kv,d_h,block,top_k,first,last,vis,dtype", [
+    (1, 1, 1, 1, 1, 32, 32, 1, 0, 0, "all", "bf16"), (1, 1, 5000, 8, 2, 128, 64, 8, 1, 1, "all", "bf16"),
+    (7, 1, 3001, 12, 3, 64, 32, 16, 1, 2, "ragged", "bf16"), (1, 130, 2100, 4, 4, 64, 32, 7, 0, 0, "causal", "bf16"),
+    (2, 70, 900, 6, 2, 256, 64, 5, 1, 1, "causal", "bf16"), (1, 90, 60, 2, 1, 32, 32, 40, 0, 1, "causal", "bf16"),
+    (2, 33, 70000, 2, 2, 32, 32, 20, 0, 0, "ragged", "bf16"), (3, 40, 1111, 16, 1, 128, 128, 3, 1, 2, "ragged", "bf16"),
+    (1, 65, 4100, 4, 4, 64, 32, 16, 0, 0, "all", "f32"), (4, 3, 1500, 10, 2, 128, 64, 9, 2, 3, "ragged", "f32"),
+    (1, 20, 2000, 3, 3, 256, 256, 4, 0, 1, "causal", "f32"), (1, 5, 20000, 2, 1, 32, 32, 256, 3, 3, "causal", "bf16")])
+def test_block_select(n_obj, n_q, n_kv, H, H_kv, d_h, block, top_k, first, last, vis, dtype):
+    run_select(n_obj, n_q, n_kv, H, H_kv, d_h, block, top_k, first, last, vis, dtype, seed=n_q + n_kv)
+
+
+def all_zero(rng, Q, M):
+    return Q * 0, M
+
+
+def equal_means(rng, Q, M):
+    return Q, np.ascontiguousarray(np.broadcast_to(M[:, :, :1], M.shape))
+
+
+def few_values(rng, Q, M):
+    """Small whole numbers: exact scores with many ties."""
+    one = lambda a: to_storage(rng.integers(-1, 2, a.shape).astype(np.float32), "bf16")  # noqa: E731
+    return one(Q), one(M)
+
+
+def close_scores(rng, Q, M):
+    """Mean keys that differ in one channel's last bits: gaps far below what
+    fp32 sums of the products can tell apart."""
+    m = np.broadcast_to(M[:, :, :1], M.shape).copy()
+    m[..., 0] = (m[..., 0] & 0xFF80) + rng.integers(0, 100, m.shape[:-1]).astype(np.uint16)
+    q = Q.copy()
+    q[..., 0] = to_storage(np.full(q.shape[:-1], 2.0 ** -12, np.float32), "bf16")
+    return q, m
+
+
+def not_finite(rng, Q, M):
+    m, q = M.copy(), Q.copy()
+    m[:, :, 3::7] = 0x7FC0        # NaN
+    m[:, :, 4::9, 1] = 0x7F80     # +inf
+    q[:, ::5] = 0xFF80            # -inf
+    return q, m
+
+
+def huge(rng, Q, M):
+    """Products past the fp32 range, sums within the fp64 range."""
+    big = lambda a, e: to_storage(np.clip(storage_to_f64(a, "bf16") * 2.0 ** e, -3e38, 3e38).astype(np.float32), "bf16")  # noqa: E731
+    return big(Q, 100), big(M, 90)
+
+
+def tiny(rng, Q, M):
+    """Products below the fp32 range."""
+    small = lambda a, e: to_storage((storage_to_f64(a, "bf16") * 2.0 ** e).astype(np.float32), "bf16")  # noqa: E731
+    return small(Q, -80), small(M, -90)
+
+
+@pytest.mark.parametrize("make", [all_zero, equal_means, few_values, close_scores, not_finite, huge, tiny])
+@pytest.mark.parametrize("n_kv", [1500, 50000])
+def test_block_select_hard_scores(make, n_kv):
+    run_select(2, 37, n_kv, 4, 2, 64, 32, 11, 1, 1, "ragged", "bf16", seed=n_kv, make=make)
+
+
+def test_block_select_nothing_to_read():
+    p = rs3()
+    s = p.block_shape(p.RS3_BF16, 2, 3, 0, 4, 2, 64, 32, 4)
+    idx = torch.full((2, 3, 2, 4), 77, dtype=torch.int32, device="cuda")
+    count = torch.full((2, 3, 2), 77, dtype=torch.int32, device="cuda")
+    Q = torch.zeros((2, 3, 4, 64), dtype=torch.bfloat16, device="cuda")
+    ws = torch.empty(max(p.block_select_workspace_size(s), 16), dtype=torch.uint8, device="cuda")
+    p.block_select(s, Q, torch.empty(0, dtype=torch.bfloat16, device="cuda"), idx, count, ws=ws)
+    torch.cuda.synchronize()
+    assert (idx == -1).all() and (count == 0).all()
+
+
+# ---- attend --------------------------------------------------------------------
+def lists(rng, n_obj, n_q, H_kv, nb, top_k, wrong):
+    """Ascending random lists of random lengths; with `wrong` some entries
+    repeat, fall back or leave the range, and counts leave [0, top_k]."""
+    idx = np.full((n_obj, n_q, H_kv, top_k), -1, np.int32)
+    count = np.zeros((n_obj, n_q, H_kv), np.int32)
+    for at in np.ndindex(n_obj, n_q, H_kv):
+        k = int(rng.integers(0, min(top_k, nb) + 1)) if rng.random() < 0.5 else min(top_k, nb)
+        idx[at][:k] = np.sort(rng.choice(nb, k, replace=False)) if k else 0
+        count[at] = k
+        if wrong and k:
+            r = rng.random()
+            if r < 0.3:
+                idx[at][rng.integers(0, k)] = rng.choice([-3, nb, nb + 5, 2 ** 31 - 1, -2 ** 31])
+            elif r < 0.6:
+                idx[at][rng.integers(0, k)] = idx[at][0]
+            elif r < 0.8:
+                count[at] = rng.choice([-4, top_k + 9])
+    return idx, count
+
+
+def check_attend(got, Q, K, V, idx, count, v, block, dtype, lists_of=None):
+    O, A, L = B.block_attend(Q, K, V, idx, count, v, block)
+    d_h, n = Q.shape[-1], idx.shape[-1] * block
+    delta = ((d_h + 4) * 2.0 ** -24 + 2.0 ** -22) * (L + 1)
+    uw, up = (2.0 ** -8, 2.0 ** -11) if dtype == "bf16" else (0.0, 0.0)
+    tol = (2 * delta + 2 * uw + up + n * 2.0 ** -24) * A + U[dtype] * np.abs(O) + 1e-30
+    bad = np.abs(got - O) - tol
+    assert (bad <= 0).all(), (np.unravel_index(bad.argmax(), bad.shape), bad.max())
+    return O
+
+
+def run_attend(n_obj, n_q, n_kv, H, H_kv, d_h, block, top_k, vis, dtype, seed, wrong=False, edit=None, strided=False,
+               shared=False):
+    p = rs3()
+    rng = np.random.default_rng(seed)
+    nb = -(-n_kv // block)
+    k_obj = 1 if shared else n_obj
+    Q = draw(rng, (n_obj, n_q, H, d_h), dtype, 1.5)
+    K, V = draw(rng, (k_obj, n_kv, H_kv, d_h), dtype), draw(rng, (k_obj, n_kv, H_kv, d_h), dtype)
+    idx, count = lists(rng, n_obj, n_q, H_kv, nb, top_k, wrong)
+    v = lengths(rng, n_obj, n_q, n_kv, vis)
+    if edit is not None:
+        Q, K, V = edit(rng, Q, K, V, v)
+    kw = {}
+    Qd, Kd, Vd = dev(Q), dev(K), dev(V)
+    if strided:   # one row per token: queries, keys and values side by side; O's objects interleaved
+        w = (H + 2 * H_kv) * d_h
+        rows = max(n_q, n_kv)
+        buf = torch.full((n_obj, rows, w), float("nan"), dtype=Qd.dtype, device="cuda")
+        buf[:, :n_q, :H * d_h] = Qd.view(n_obj, n_q, -1)
+        buf[:, :n_kv, H * d_h:(H + H_kv) * d_h] = Kd.view(n_obj, n_kv, -1)
+        buf[:, :n_kv, (H + H_kv) * d_h:] = Vd.view(n_obj, n_kv, -1)
+        Qd, Kd, Vd = buf, buf[:, :, H * d_h:], buf[:, :, (H + H_kv) * d_h:]
+        kw = {x + y: z for x in "qkv" for y, z in (("_stride", w), ("_obj_stride", rows * w))}
+        kw.update(o_stride=n_obj * H * d_h, o_obj_stride=H * d_h)
+    if shared:
+        kw.update(k_obj_stride=0, v_obj_stride=0)
+    s = p.block_shape(dt_of(dtype), n_obj, n_q, n_kv, H, H_kv, d_h, block, top_k, **kw)
+    O = torch.full((n_q, n_obj, H, d_h) if strided else (n_obj, n_q, H, d_h), float("nan"), dtype=Qd.dtype, device="cuda")
+    ws = torch.full((max(p.block_attend_workspace_size(s), 16),), 0xFF, dtype=torch.uint8, device="cuda")
+    p.block_attend(s, Qd, Kd, Vd, dev(idx), dev(count), O, n_vis=None if v is None else dev(v), ws=ws)
+    torch.cuda.synchronize()
+    got = host(O.transpose(0, 1).contiguous() if strided else O, dtype)
+    Kf, Vf = storage_to_f64(K, dtype), storage_to_f64(V, dtype)
+    if shared:
+        Kf, Vf = (np.broadcast_to(a, (n_obj,) + a.shape[1:]) for a in (Kf, Vf))
+    return got, (storage_to_f64(Q, dtype), Kf, Vf, idx, count,
+                 np.full((n_obj, n_q), n_kv) if v is None else v, block, dtype)
+
+
+ATTEND = [
+    (1, 1, 1, 1, 1, 32, 32, 1, "all", "bf16"), (1, 1, 4000, 8, 1, 128, 64, 8, "all", "bf16"),
+    (5, 1, 1000, 12, 4, 64, 32, 9, "ragged", "bf16"), (3, 2, 700, 16, 1, 128, 64, 4, "causal", "bf16"),
+    (2, 1, 900, 40, 2, 32, 128, 3, "ragged", "bf16"), (9, 1, 300, 5, 5, 256, 64, 2, "ragged", "bf16"),
+    (1, 200, 1500, 2, 2, 128, 64, 8, "all", "bf16"), (1, 300, 700, 4, 4, 32, 32, 6, "causal", "bf16"),
+    (2, 150, 333, 6, 2, 64, 32, 5, "ragged", "bf16"), (1, 129, 2100, 10, 2, 128, 128, 4, "causal", "bf16"),
+    (1, 100, 600, 3, 1, 256, 64, 3, "causal", "bf16"), (2, 90, 1030, 7, 1, 64, 256, 3, "ragged", "bf16"),
+    (1, 260, 50, 4, 4, 64, 32, 3, "causal", "bf16"), (1, 70, 5000, 1, 1, 256, 256, 9, "ragged", "bf16"),
+    (1, 1, 500, 4, 2, 64, 32, 6, "all", "f32"), (4, 3, 400, 6, 2, 128, 64, 4, "ragged", "f32"),
+    (1, 150, 600, 4, 4, 64, 32, 8, "causal", "f32"), (1, 80, 500, 5, 1, 32, 128, 3, "ragged", "f32"),
+    (2, 70, 300, 2, 2, 256, 64, 3, "causal", "f32"), (1, 64, 300, 8, 4, 128, 256, 2, "all", "f32")]
+
+
+@pytest.mark.parametrize("n_obj,n_q,n_kv,H,H_kv,d_h,block,top_k,vis,dtype", ATTEND)
+def test_block_attend(n_obj, n_q, n_kv, H, H_kv, d_h, block, top_k, vis, dtype):
+    got, args = run_attend(n_obj, n_q, n_kv, H, H_kv, d_h, block, top_k, vis, dtype, seed=n_q + n_kv + d_h)
+    check_attend(got, *args)
+
+
+@pytest.mark.parametrize("case", [1, 2, 6, 8, 14, 16])
+@pytest.mark.parametrize("kw", [dict(wrong=True), dict(strided=True), dict(shared=True)])
+def test_block_attend_lists_and_layouts(case, kw):
+    got, args = run_attend(*ATTEND[case], seed=case, **kw)
+    check_attend(got, *args)
+
+
+def unseen_garbage(rng, Q, K, V, v):
+    """NaN and Inf in keys and values that nobody, or only later queries, see."""
+    top = int(np.max(np.clip(v, 0, K.shape[1])))
+    for a in (K, V):
+        nan, inf = (0x7FC0, 0x7F80) if a.dtype == np.uint16 else (np.nan, np.inf)
+        a[:, top:] = nan
+        a[:, top + 1::2] = inf
+    return Q, K, V
+
+
+@pytest.mark.parametrize("case", [2, 3, 7, 8, 9, 11, 15, 16])
+def test_block_attend_masked_garbage(case):
+    c = list(ATTEND[case])
+    c[2] += 70
+    if c[8] == "causal":
+        # every query stops short of the last keys
+        def edit(rng, Q, K, V, v):
+            v -= 75
+            return unseen_garbage(rng, Q, K, V, v)
+    else:
+        def edit(rng, Q, K, V, v):
+            np.minimum(v, K.shape[1] - 40, out=v)
+            return unseen_garbage(rng, Q, K, V, v)
+    got, args = run_attend(*c, seed=case + 50, edit=edit)
+    Q, K, V = args[0], np.nan_to_num(args[1], posinf=0, neginf=0), np.nan_to_num(args[2], posinf=0, neginf=0)
+    check_attend(got, Q, K, V, *args[3:])
+
+
+@pytest.mark.parametrize("dtype,d_h,G", [("bf16", 64, 1), ("bf16", 128, 4), ("f32", 64, 2)])
+def test_block_attend_garbage_seen_by_later_queries(dtype, d_h, G):
+    """A query must not meet the Inf or NaN of a key that only later queries of
+    the same block see; those queries get what the formula gives, no number."""
+    n_q = 96
+    def edit(rng, Q, K, V, v):
+        V[0, 70, 0, 3] = 0x7FC0 if dtype == "bf16" else np.nan
+        V[0, 80, 0, 5] = 0x7F80 if dtype == "bf16" else np.inf
+        K[0, 85, 0, 7] = 0x7FC0 if dtype == "bf16" else np.nan
+        return Q, K, V
+    got, args = run_attend(1, n_q, n_q, G, 1, d_h, 64, 2, "causal", dtype, seed=9, edit=edit)
+    Q, K, V, idx, count, v, block, _ = args
+    reads = np.array([1 in B.valid_blocks(idx[0, i, 0], count[0, i, 0], 2) for i in range(n_q)])
+    early = (v[0] <= 70) | ~reads
+    check_attend(got[:, early], Q[:, early], np.nan_to_num(K), np.nan_to_num(V, posinf=0), idx[:, early],
+                 count[:, early], v[:, early], block, dtype)
+    late = reads & (v[0] > 85)
+    assert late.any() and np.isnan(got[0, late]).all()
+    mid = reads & (v[0] > 70) & (v[0] <= 80)
+    assert mid.any() and np.isnan(got[0, mid][..., 3]).all() and np.isfinite(got[0, mid][..., :3]).all()
+
+
+def test_block_attend_extreme_logits():
+    """Logits of -inf have weight 0, a row of them gives 0, and logits that
+    rise from block to block move the softmax's reference."""
+    def edit(rng, Q, K, V, v):
+        q, k = storage_to_f64(Q, "bf16"), storage_to_f64(K, "bf16")
+        k[..., 0] = 0
+        q[..., 0] = 0
+        q[:, :, :, 1] = 8.0
+        k[:, :, :, 1] = (np.arange(k.shape[1]) * 0.7)[None, :, None]     # rising along the keys
+        k[:, 64:96] *= 0
+        k[:, 64:96, :, 1] = -3e38                                          # overflow to -inf
+        return to_storage(q.astype(np.float32), "bf16"), to_storage(k.astype(np.float32), "bf16"), V
+    for n_q in (1, 130):
+        got, args = run_attend(1, n_q, 320, 2, 2, 64, 32, 10, "all", "bf16", seed=n_q, edit=edit)
+        assert np.isfinite(got).all()
+        Q, K, V, idx, count, v, block, _ = args
+        for i in range(n_q):
+            for g in range(2):
+                if B.valid_blocks(idx[0, i, g], count[0, i, g], 10) == [2]:
+                    idx[0, i, g] = -1
+        Kc = K.copy()
+        Kc[:, 64:96, :, 1] = -1e6      # weight 0 in fp64 too
+        check_attend(got, Q, Kc, V, idx, count, v, block, "bf16")
+
+
+# ---- together --------------------------------------------------------------------
+def test_run_of_all_calls_on_a_growing_cache():
+    """Norm and rotation into the cache, the newest block's mean, the choice and
+    the attention, token by token on another stream, against the same calls
+    made of the whole prompt at once."""
+    p = rs3()
+    gen = torch.Generator(device="cuda").manual_seed(5)
+    n_obj, n, H, H_kv, d_h, block, top_k = 2, 150, 4, 2, 64, 32, 3
+    q = torch.randn((n_obj, n, H, d_h), generator=gen, device="cuda").bfloat16()
+    k = torch.randn((n_obj, n, H_kv, d_h), generator=gen, device="cuda").bfloat16()
+    V = torch.randn((n_obj, n, H_kv, d_h), generator=gen, device="cuda").bfloat16()
+    a = torch.arange(n, device="cuda")[:, None] * 0.3 ** torch.arange(d_h // 2, device="cuda")
+    table = torch.stack([a.cos(), a.sin()], -1).float().contiguous()
+    dt, nb = p.RS3_BF16, -(-n // block)
+
+    def buffers(n_q):
+        s = p.block_shape(dt, n_obj, n_q, n, H, H_kv, d_h, block, top_k, 1, 1)
+        i32 = dict(dtype=torch.int32, device="cuda")
+        ws = torch.empty(max(p.block_select_workspace_size(s), p.block_attend_workspace_size(s), 16),
+                         dtype=torch.uint8, device="cuda")
+        return s, torch.zeros((n_obj, n_q, H_kv, top_k), **i32), torch.zeros((n_obj, n_q, H_kv), **i32), ws
+
+    Qn, Kn = torch.zeros_like(q), torch.zeros_like(k)
+    for o in range(n_obj):
+        p.qk_norm_rope(n, q[o], H, k[o], H_kv, d_h, dt, Qn[o], Kn[o], table=table, d_rot=d_h, pairing=1)
+    s, idx, count, ws = buffers(n)
+    vis = (torch.arange(n, device="cuda", dtype=torch.int32) + 1).expand(n_obj, n).contiguous()
+    means = torch.zeros((n_obj, H_kv, nb, d_h), dtype=torch.bfloat16, device="cuda")
+    O = torch.zeros_like(q)
+    p.block_means(s, Kn, means)
+    p.block_select(s, Qn, means, idx, count, n_vis=vis, ws=ws)
+    p.block_attend(s, Qn, Kn, V, idx, count, O, n_vis=vis, ws=ws)
+    torch.cuda.synchronize()
+
+    st = torch.cuda.Stream()
+    with torch.cuda.stream(st):
+        s1, idx1, count1, ws1 = buffers(1)
+        Q1, K1, means1, O1 = torch.zeros_like(q), torch.zeros_like(k), torch.zeros_like(means), torch.zeros_like(q)
+        o1 = torch.zeros((n_obj, 1, H, d_h), dtype=torch.bfloat16, device="cuda")
+        rows = []
+        for t in range(n):
+            for o in range(n_obj):
+                p.qk_norm_rope(1, q[o, t], H, k[o, t], H_kv, d_h, dt, Q1[o, t], K1[o, t], table=table, d_rot=d_h,
+                               pairing=1, pos=vis[o, t:t + 1] - 1)
+            length = vis[:, t].contiguous()
+            p.block_means(s1, K1, means1, kv_len=length, n_new=1)
+            p.block_select(s1, Q1[:, t].contiguous(), means1, idx1, count1, n_vis=length, ws=ws1)
+            p.block_attend(s1, Q1[:, t].contiguous(), K1, V, idx1, count1, o1, n_vis=length, ws=ws1)
+            O1[:, t] = o1[:, 0]
+            rows.append((idx1.clone(), count1.clone()))
+    st.synchronize()
+    assert torch.equal(Qn, Q1) and torch.equal(Kn, K1) and torch.equal(means, means1)
+    # the scores of a row that is still inside a block go by other means than the
+    # whole prompt's, but the block that a query ends in is forced, so the lists agree
+    for t in range(n):
+        assert torch.equal(rows[t][0][:, 0], idx[:, t]) and torch.equal(rows[t][1][:, 0], count[:, t])
+    f = lambda x: host(x, "bf16")  # noqa: E731
+    args = (f(Qn), f(Kn), f(V), idx.cpu().numpy(), count.cpu().numpy(), vis.cpu().numpy(), block, "bf16")
+    check_attend(f(O), *args)
+    check_attend(f(O1), *args)
+
+
+def test_captured_calls_replay():
+    """The three calls in a graph, replayed on new inputs between eager calls."""
+    p = rs3()
+    n_obj, n_q, n_kv, H, H_kv, d_h, block, top_k = 1, 200, 1000, 4, 2, 64, 32, 6
+    for n_q in (1, 200):
+        s = p.block_shape(p.RS3_BF16, n_obj, n_q, n_kv, H, H_kv, d_h, block, top_k, 1, 1)
+        Q = torch.zeros((n_obj, n_q, H, d_h), dtype=torch.bfloat16, device="cuda")
+        K, V = (torch.zeros((n_obj, n_kv, H_kv, d_h), dtype=torch.bfloat16, device="cuda") for _ in range(2))
+        nb = -(-n_kv // block)
+
+        def outputs():
+            need = max(p.block_select_workspace_size(s), p.block_attend_workspace_size(s), 16)
+            return (torch.zeros((n_obj, H_kv, nb, d_h), dtype=torch.bfloat16, device="cuda"),
+                    torch.zeros((n_obj, n_q, H_kv, top_k), dtype=torch.int32, device="cuda"),
+                    torch.zeros((n_obj, n_q, H_kv), dtype=torch.int32, device="cuda"), torch.zeros_like(Q),
+                    torch.empty(need, dtype=torch.uint8, device="cuda"))
+
+        def calls(out):
+            M, idx, count, O, ws = out
+            p.block_means(s, K, M)
+            p.block_select(s, Q, M, idx, count, ws=ws)
+            p.block_attend(s, Q, K, V, idx, count, O, ws=ws)
+
+        a, b = outputs(), outputs()
+        calls(a)
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            calls(a)
+        for r in range(4):
+            for x in (Q, K, V):
+                x.normal_()
+            graph.replay()
+            calls(b)
+            torch.cuda.synchronize()
+            for x, y in zip(a[:4], b[:4]):
+                assert torch.equal(x, y), r
