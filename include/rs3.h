@@ -470,7 +470,8 @@ rs3_status rs3_qk_norm_rope(int32_t n, const void* Q, int64_t q_stride, int32_t 
  * x_stride, x_obj_stride (elements) for x = q, k, v, o: row i of object o
  *           starts at o * x_obj_stride + i * x_stride and holds the heads one
  *           after the other.  A q, k or v object stride of 0 is one tensor
- *           shared by all objects.  O's rows must not overlap.
+ *           shared by all objects.  O's rows must not overlap; k_stride and
+ *           v_stride are below 2^22.
  * n_vis   : device int32 [n_obj][n_q], how many of its object's first keys each
  *           query sees (values are taken into [0, n_kv]), NULL for all n_kv.
  *           Causal prompts, caches of different lengths and padded rows (0)

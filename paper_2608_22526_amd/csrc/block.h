@@ -2,7 +2,7 @@
 // of the norm and rotation of queries and keys.
 #pragma once
 
-#include "device_util.h"
+#include "attn_util.h"
 
 namespace rs3 {
 
@@ -51,9 +51,59 @@ struct BlockAttendArgs {
   int n_obj, n_q, n_kv, H, H_kv, G, d_h, block, n_blk, top_k;
 };
 
+// Blocks of keys that the counters of the tiled attention hold.
+constexpr int BLOCK_TILE_MAX = 8192;
+
+// Workspace of the tiled attention for one run of queries (i0 .. i0 + nq of
+// every object); a group is an (object, key head) pair.
+struct BlockTile {
+  int b, part;             // block, and which 128 of its (query, head) rows
+  int start, cnt;          // the block's queries in the group's list
+};
+struct BlockTileArgs {
+  uint32_t* ord;           // [groups][nq][top_k] place of an entry among its run's queries of that block, ~0: none
+  uint32_t* hist;          // [runs][groups][n_blk] queries of each run that list the block
+  uint32_t* list;          // [groups][nq * top_k] query * top_k + slot, by block
+  BlockTile* tiles;        // [groups][tcap]
+  int32_t* ntiles;         // [groups]
+  int i0, nq, tcap, groups, runs, run;   // run: queries of one counting work-group
+};
+
+// Partial rows, merged by k_block_merge: row ((o * nq + i) * H_kv + g) * S + s)
+// * G + head of [d_h] values and (m, l) pairs; s is a slot of the list (tiled
+// form) or a split of the keys.
+struct BlockPartArgs {
+  void* Opart;
+  float* ML;
+  int S, i0, nq;
+};
+
 // How many keys query `i` (of all objects' queries) sees.
 __device__ __forceinline__ int visible_keys(const int32_t* n_vis, int64_t i, int n_kv) {
   return n_vis ? min(max(gload(n_vis + i), 0), n_kv) : n_kv;
+}
+
+// LDS layout of a stage of key (value) rows: 16-byte chunk c of row r lies at
+// chunk c ^ f(r) of the row, so that the rows that one LDS cycle reads fall on
+// different banks.  CPR chunks a row; 16 / CPR rows share the 256 bytes of one
+// cycle.  k: 16 (or more) keys at one chunk.  v: WD neighbouring chunks of the
+// rows whose number differs in the bits from SH up.
+template <int CPR>
+struct Swz {
+  static constexpr int RPB = CPR >= 16 ? 1 : 16 / CPR, W = CPR >= 16 ? 16 : CPR;
+  static __device__ __forceinline__ int k(int r) { return (r / RPB) & (W - 1); }
+  template <int WD, int SH>
+  static __device__ __forceinline__ int v(int r) {
+    return (((r >> SH) / (SH ? 1 : RPB)) & (W / WD - 1)) * WD;
+  }
+};
+
+// Value operand of a bf16 product from rows of keys: lane i of 16 gets the four
+// values of channel i of four keys; lane s supplies the address of channels
+// 4 (s % 4) .. +3 of key s / 4.
+__device__ __forceinline__ u32x2 lds_tr4(const uint8_t* p) {
+  typedef short s16x4 __attribute__((ext_vector_type(4)));
+  return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)p));
 }
 
 template <class T>
@@ -72,4 +122,10 @@ __device__ __forceinline__ T from_f32(float v) {
 hipError_t rs3_launch_qk_norm(const rs3::QkNormArgs& a, int dtype, hipStream_t st);
 hipError_t rs3_launch_block_means(const rs3::BlockMeansArgs& a, int n_obj, int dtype, hipStream_t st);
 hipError_t rs3_launch_block_select(const rs3::BlockSelectArgs& a, int dtype, hipStream_t st);
-hipError_t rs3_launch_block_attend(const rs3::BlockAttendArgs& a, int dtype, hipStream_t st);
+hipError_t rs3_launch_block_row(const rs3::BlockAttendArgs& a, const rs3::BlockPartArgs& w, int dtype, hipStream_t st);
+hipError_t rs3_launch_block_tile(const rs3::BlockAttendArgs& a, const rs3::BlockTileArgs& t,
+                                 const rs3::BlockPartArgs& w, int dtype, hipStream_t st);
+hipError_t rs3_launch_block_merge(const rs3::BlockAttendArgs& a, const rs3::BlockPartArgs& w, int dtype, bool f16,
+                                  hipStream_t st);
+hipError_t rs3_block_setup();
+hipError_t rs3_block_tile_setup();

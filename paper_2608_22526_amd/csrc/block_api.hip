@@ -38,6 +38,11 @@ bool rows_ok(const rs3_block_shape* s, int64_t row, int64_t obj, int heads) {
   return stride_ok(row, es) && stride_ok(obj, es) && row >= (int64_t)heads * s->d_h;
 }
 
+// The attention's lanes add up the row offsets of a block in 32 bits.
+bool kv_rows_ok(const rs3_block_shape* s, int64_t row, int64_t obj) {
+  return rows_ok(s, row, obj, s->H_kv) && row < (1 << 22);
+}
+
 bool out_rows_ok(const rs3_block_shape* s) {
   const int64_t w = (int64_t)s->H * s->d_h;
   if (!rows_ok(s, s->o_stride, s->o_obj_stride, s->H)) return false;
@@ -47,6 +52,73 @@ bool out_rows_ok(const rs3_block_shape* s) {
 }
 
 int n_blocks(const rs3_block_shape* s) { return (s->n_kv + s->block - 1) / s->block; }
+
+size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
+
+// How a call of rs3_block_attend runs.
+struct AttendPlan {
+  bool tile;         // tiled form, in runs of `step` queries of every object
+  int step, S;       // S: splits of a row's keys (other form)
+  int groups, runs, run, tcap;
+  size_t ord, hist, list, tiles, ntiles, opart, ml, total;
+};
+
+constexpr int TROWS = 128;   // of block_tile.hip
+constexpr size_t PART_BYTES = (size_t)640 << 20;   // partial rows of one run of queries
+
+void attend_plan(const rs3_block_shape* s, AttendPlan* a) {
+  memset(a, 0, sizeof(*a));
+  const int n_blk = (s->n_kv + s->block - 1) / s->block, G = s->H / s->H_kv;
+  size_t off = 0;
+  auto take = [&](size_t bytes) {
+    const size_t at = off;
+    off += align256(bytes);
+    return at;
+  };
+  a->tile = s->n_q >= 64 && n_blk <= BLOCK_TILE_MAX && n_blk > 0;
+  if (a->tile) {
+    const size_t per_q = (size_t)s->n_obj * s->H * s->top_k * (s->d_h * elem(s->dt) + 8);
+    const int64_t most_q = std::max<int64_t>(512, (int64_t)(PART_BYTES / per_q)), parts = (s->n_q + most_q - 1) / most_q;
+    a->step = (int)((s->n_q + parts - 1) / parts);
+    a->groups = s->n_obj * s->H_kv;
+    // every scattering work-group adds up the counts of all runs
+    int most = 65536 / n_blk;
+    most = most < 4 ? 4 : most > 64 ? 64 : most;
+    a->run = (a->step + most - 1) / most;
+    if (a->run < 64) a->run = 64;
+    a->runs = (a->step + a->run - 1) / a->run;
+    const int64_t entries = (int64_t)a->step * s->top_k;
+    a->tcap = (int)(entries * G / TROWS + (n_blk < entries ? n_blk : entries));
+    a->ord = take(entries * a->groups * 4);
+    a->hist = take((size_t)a->runs * a->groups * n_blk * 4);
+    a->list = take(entries * a->groups * 4);
+    a->tiles = take((size_t)a->tcap * a->groups * sizeof(BlockTile));
+    a->ntiles = take((size_t)a->groups * 4);
+    a->opart = take(entries * s->H * s->n_obj * s->d_h * elem(s->dt));
+    a->ml = take(entries * s->H * s->n_obj * 8);
+  } else {
+    // work-groups for the chip twice over, each with a few pieces of 32 keys per wave
+    const int64_t rows = (int64_t)s->n_obj * s->n_q * s->H_kv * ((G + 15) / 16);
+    int64_t S = rows > 0 ? 512 / rows : 1;
+    const int64_t most = (int64_t)s->top_k * s->block / 32 / 8;
+    S = S < most ? S : most;
+    a->S = (int)(S < 1 ? 1 : S);
+    if (a->S > 1) {
+      a->opart = take((size_t)s->n_obj * s->n_q * s->H * a->S * s->d_h * 4);
+      a->ml = take((size_t)s->n_obj * s->n_q * s->H * a->S * 8);
+    }
+  }
+  a->total = off;
+}
+
+bool setup_done = false;
+
+rs3_status ensure_setup() {
+  if (setup_done) return RS3_OK;
+  if (rs3_block_setup() != hipSuccess) return RS3_E_DEVICE;
+  setup_done = true;
+  return RS3_OK;
+}
 
 size_t select_ws(const rs3_block_shape* s) {
   return (size_t)s->n_obj * s->n_q * s->H_kv * n_blocks(s) * sizeof(double);
@@ -107,7 +179,7 @@ rs3_status rs3_qk_norm_rope(int32_t n, const void* Q, int64_t q_stride, int32_t 
 
 rs3_status rs3_block_means(const rs3_block_shape* s, const void* K, const int32_t* kv_len, int32_t n_new, void* Kmean,
                            void* stream) {
-  if (!shape_ok(s) || n_new < 0 || !rows_ok(s, s->k_stride, s->k_obj_stride, s->H_kv)) return RS3_E_INVALID;
+  if (!shape_ok(s) || n_new < 0 || !kv_rows_ok(s, s->k_stride, s->k_obj_stride)) return RS3_E_INVALID;
   if (!aligned16(K) || !aligned16(Kmean) || (s->n_kv > 0 && (!K || !Kmean))) return RS3_E_INVALID;
   if (s->n_kv == 0) return RS3_OK;
   BlockMeansArgs a;
@@ -167,7 +239,9 @@ rs3_status rs3_block_select(const rs3_block_shape* s, const void* Q, const void*
 
 rs3_status rs3_block_attend_workspace_size(const rs3_block_shape* s, size_t* bytes) {
   if (!bytes || !shape_ok(s)) return RS3_E_INVALID;
-  *bytes = 0;
+  AttendPlan pl;
+  attend_plan(s, &pl);
+  *bytes = pl.total;
   return RS3_OK;
 }
 
@@ -175,13 +249,17 @@ rs3_status rs3_block_attend(const rs3_block_shape* s, const void* Q, const void*
                             const int32_t* count, const int32_t* n_vis, void* O, void* ws, size_t ws_bytes,
                             void* stream) {
   if (!shape_ok(s) || !rows_ok(s, s->q_stride, s->q_obj_stride, s->H) ||
-      !rows_ok(s, s->k_stride, s->k_obj_stride, s->H_kv) || !rows_ok(s, s->v_stride, s->v_obj_stride, s->H_kv) ||
-      !out_rows_ok(s))
+      !kv_rows_ok(s, s->k_stride, s->k_obj_stride) || !kv_rows_ok(s, s->v_stride, s->v_obj_stride) || !out_rows_ok(s))
     return RS3_E_INVALID;
   if (!aligned16(Q) || !aligned16(K) || !aligned16(V) || !aligned16(O) || !aligned16(ws)) return RS3_E_INVALID;
   if (s->n_q == 0) return RS3_OK;
   if (!Q || !idx || !count || !O || (s->n_kv > 0 && (!K || !V))) return RS3_E_INVALID;
   if (O == Q || (s->n_kv > 0 && (O == K || O == V))) return RS3_E_INVALID;
+  AttendPlan pl;
+  attend_plan(s, &pl);
+  if (pl.total > 0 && (!ws || ws_bytes < pl.total)) return RS3_E_INVALID;
+  const rs3_status st0 = ensure_setup();
+  if (st0 != RS3_OK) return st0;
   BlockAttendArgs a;
   memset(&a, 0, sizeof(a));
   a.Q = Q;
@@ -210,7 +288,39 @@ rs3_status rs3_block_attend(const rs3_block_shape* s, const void* Q, const void*
   a.block = s->block;
   a.n_blk = n_blocks(s);
   a.top_k = s->top_k;
-  return map_err(rs3_launch_block_attend(a, s->dt, (hipStream_t)stream));
+  const hipStream_t st = (hipStream_t)stream;
+  uint8_t* w = (uint8_t*)ws;
+  BlockPartArgs part;
+  memset(&part, 0, sizeof(part));
+  part.Opart = w + pl.opart;
+  part.ML = (float*)(w + pl.ml);
+  if (!pl.tile) {
+    part.S = pl.S;
+    part.nq = s->n_q;
+    hipError_t e = rs3_launch_block_row(a, part, s->dt, st);
+    if (e == hipSuccess && pl.S > 1) e = rs3_launch_block_merge(a, part, s->dt, false, st);
+    return map_err(e);
+  }
+  BlockTileArgs t;
+  memset(&t, 0, sizeof(t));
+  t.ord = (uint32_t*)(w + pl.ord);
+  t.hist = (uint32_t*)(w + pl.hist);
+  t.list = (uint32_t*)(w + pl.list);
+  t.tiles = (BlockTile*)(w + pl.tiles);
+  t.ntiles = (int32_t*)(w + pl.ntiles);
+  t.run = pl.run;
+  t.tcap = pl.tcap;
+  t.groups = pl.groups;
+  part.S = s->top_k;
+  hipError_t e = hipSuccess;
+  for (int i0 = 0; i0 < s->n_q && e == hipSuccess; i0 += pl.step) {
+    part.i0 = t.i0 = i0;
+    part.nq = t.nq = s->n_q - i0 < pl.step ? s->n_q - i0 : pl.step;
+    t.runs = (t.nq + pl.run - 1) / pl.run;
+    e = rs3_launch_block_tile(a, t, part, s->dt, st);
+    if (e == hipSuccess) e = rs3_launch_block_merge(a, part, s->dt, true, st);
+  }
+  return map_err(e);
 }
 
 }  // extern "C"

@@ -1,0 +1,500 @@
+// Block-sparse attention of many queries: the lists are turned round, so that
+// a work-group holds one block of keys and values in LDS and computes it for
+// 128 of the (query, head) rows that list it.
+//
+//  k_block_count, k_block_scatter : the queries of every block, and the tiles;
+//  k_block_tile  : softmax and value product of one block for 128 rows, a
+//                  partial row (m, l, O) for each;
+//  k_block_merge : the partials of a query joined.
+//
+// A query-major form reads its blocks anew for every query (64 KB of L2 for 64
+// keys of 128 channels and one query head); here a block is read once per 128
+// rows, and what moves is a row of Q and a partial row for every (query, head,
+// listed block).
+#include "block.h"
+
+namespace rs3 {
+
+typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
+
+constexpr int TROWS = 128;  // rows of a tile, 32 per wave
+
+// grid (runs, groups), 512 threads, n_blk counters in LDS.  Entries that take
+// no part (out of range, not ascending, past the count, not seen) get no place
+// and an empty partial.
+__global__ __launch_bounds__(512) void k_block_count(BlockAttendArgs p, BlockTileArgs w, BlockPartArgs part) {
+  extern __shared__ uint32_t sc[];
+  const int run = blockIdx.x, grp = blockIdx.y, o = grp / p.H_kv, hk = grp - o * p.H_kv, tid = threadIdx.x;
+  for (int b = tid; b < p.n_blk; b += 512) sc[b] = 0;
+  __syncthreads();
+  const int q0 = run * w.run, items = min(w.run, w.nq - q0) * p.top_k;
+  for (int e = tid; e < items; e += 512) {
+    const int iq = e / p.top_k, t = e - iq * p.top_k, i = q0 + iq;
+    const int64_t oi = (int64_t)o * p.n_q + w.i0 + i, row = oi * p.H_kv + hk;
+    const int32_t* list = p.idx + row * p.top_k;
+    const int b = gload(list + t), prev = gload(list + max(t - 1, 0)), cnt = min(gload(p.count + row), p.top_k);
+    const bool ok = t < cnt && b >= 0 && b < p.n_blk && (t == 0 || b > prev) &&
+                    (int64_t)b * p.block < visible_keys(p.n_vis, oi, p.n_kv);
+    uint32_t at = ~0u;
+    if (ok) {
+      at = atomicAdd(&sc[b], 1u);
+    } else {
+      float* ml = part.ML + (((((int64_t)o * w.nq + i) * p.H_kv + hk) * p.top_k + t) * p.G) * 2;
+      for (int g = 0; g < p.G; ++g) {
+        ml[2 * g] = -INFINITY;
+        ml[2 * g + 1] = 0.f;
+      }
+    }
+    w.ord[((int64_t)grp * w.nq + i) * p.top_k + t] = at;
+  }
+  __syncthreads();
+  for (int b = tid; b < p.n_blk; b += 512) w.hist[((int64_t)run * w.groups + grp) * p.n_blk + b] = sc[b];
+}
+
+// Same grid: every work-group adds up the runs' counts of its group (they are
+// few), so that no launch has to hand them on; run 0 writes the tiles.  LDS:
+// the blocks' counts and then where this run's queries of each begin.
+__global__ __launch_bounds__(512) void k_block_scatter(BlockAttendArgs p, BlockTileArgs w) {
+  extern __shared__ uint32_t sm[];
+  __shared__ uint64_t wsum[8];
+  uint32_t* pre = sm;
+  uint32_t* tot = sm + p.n_blk;
+  const int run = blockIdx.x, grp = blockIdx.y, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  for (int b = tid; b < p.n_blk; b += 512) {
+    uint32_t a = 0, t = 0;
+    for (int r0 = 0; r0 < w.runs; r0 += 8) {
+      uint32_t n[8];
+#pragma unroll
+      for (int k = 0; k < 8; ++k)
+        n[k] = gload(w.hist + ((int64_t)min(r0 + k, w.runs - 1) * w.groups + grp) * p.n_blk + b);
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        a += r0 + k < run ? n[k] : 0;
+        t += r0 + k < w.runs ? n[k] : 0;
+      }
+    }
+    pre[b] = a;
+    tot[b] = t;
+  }
+  __syncthreads();
+  // exclusive scan over the blocks of (entries << 32 | tiles), a stretch of blocks per thread
+  const int per = (p.n_blk + 511) / 512, b0 = min(tid * per, p.n_blk), b1 = min(b0 + per, p.n_blk);
+  uint64_t mine = 0;
+  for (int b = b0; b < b1; ++b) mine += ((uint64_t)tot[b] << 32) | ((tot[b] * (uint32_t)p.G + TROWS - 1) / TROWS);
+  uint64_t incl = mine;
+  for (int d = 1; d < 64; d <<= 1) {
+    const uint64_t up = __shfl_up(incl, d, 64);
+    if (lane >= d) incl += up;
+  }
+  if (lane == 63) wsum[wave] = incl;
+  __syncthreads();
+  uint64_t at = incl - mine;
+  for (int i = 0; i < wave; ++i) at += wsum[i];
+  BlockTile* tiles = w.tiles + (int64_t)grp * w.tcap;
+  for (int b = b0; b < b1; ++b) {
+    const uint32_t n = tot[b], start = (uint32_t)(at >> 32), nt = (n * (uint32_t)p.G + TROWS - 1) / TROWS;
+    pre[b] += start;
+    if (run == 0)
+      for (uint32_t t = 0; t < nt; ++t) {
+        BlockTile e;
+        e.b = b;
+        e.part = (int)t;
+        e.start = (int)start;
+        e.cnt = (int)n;
+        tiles[(uint32_t)at + t] = e;
+      }
+    at += ((uint64_t)n << 32) | nt;
+  }
+  if (run == 0 && tid == 511) w.ntiles[grp] = (int)(uint32_t)at;
+  __syncthreads();
+  const int q0 = run * w.run, items = min(w.run, w.nq - q0) * p.top_k, o = grp / p.H_kv, hk = grp - o * p.H_kv;
+  const int64_t base = (int64_t)grp * w.nq * p.top_k;
+  for (int e = tid; e < items; e += 512) {
+    const uint32_t place = gload(w.ord + base + (int64_t)q0 * p.top_k + e);
+    if (place == ~0u) continue;
+    const int iq = e / p.top_k, t = e - iq * p.top_k;
+    const int64_t row = ((int64_t)o * p.n_q + w.i0 + q0 + iq) * p.H_kv + hk;
+    w.list[base + pre[gload(p.idx + row * p.top_k + t)] + place] = (uint32_t)(q0 * p.top_k + e);
+  }
+}
+
+// The (m, l) pair of a partial whose values are f16 times 2^e (device_util.h,
+// at part_sum); a sum that is no number is handed on in m.
+__device__ __forceinline__ void encode_ml(float m, float l, int e, float* out) {
+  if (l > 0.f) {
+    const int el = __builtin_amdgcn_frexp_expf(l) - 1;
+    m += (float)el;
+    l = __builtin_amdgcn_ldexpf(l, e - el);
+  } else {
+    m = l == 0.f ? -INFINITY : NAN;
+    l = 0.f;
+  }
+  *(float2*)out = make_float2(m, l);
+}
+
+// The power of two of a row whose largest finite value is `big`: row / 2^e < 2^15.
+__device__ __forceinline__ int row_exp(float big) { return max(__builtin_amdgcn_frexp_expf(big) - 15, -126); }
+
+// One partial row by the whole wave, key by key: for rows that do not see all
+// of the block where a product with weight 0 was no number (Inf or NaN in a
+// value that the row does not see).
+template <class T, int D>
+__device__ __noinline__ void careful_row(const T* q, const T* k, int64_t ks, const T* v, int64_t vs, int keys,
+                                         float qscale, void* orow, float* ml) {
+  constexpr int E = D < 64 ? 1 : D / 64;
+  const int lane = threadIdx.x & 63;
+  const bool on = lane < D;
+  float qv[E], acc[E], m = -INFINITY, l = 0.f;
+#pragma unroll
+  for (int e = 0; e < E; ++e) {
+    qv[e] = on ? to_f32<T>(q[lane + 64 * e]) : 0.f;
+    acc[e] = 0.f;
+  }
+  for (int pass = 0; pass < 2; ++pass) {
+    const float sub = m == -INFINITY ? 0.f : m;
+    for (int j = 0; j < keys; ++j) {
+      float s = 0.f;
+#pragma unroll
+      for (int e = 0; e < E; ++e) s += on ? qv[e] * to_f32<T>(k[j * ks + lane + 64 * e]) : 0.f;
+      s = wave_sum(s) * qscale;
+      if (pass == 0) {
+        m = __builtin_elementwise_maximum(m, s);
+        continue;
+      }
+      const float w = __builtin_amdgcn_exp2f(s - sub);
+      l += w;
+      if (w == 0.f) continue;
+#pragma unroll
+      for (int e = 0; e < E; ++e) acc[e] += on ? w * to_f32<T>(v[j * vs + lane + 64 * e]) : 0.f;
+    }
+  }
+  const float inv = l > 0.f ? 1.f / l : 0.f;
+  float big = 0.f;
+#pragma unroll
+  for (int e = 0; e < E; ++e) {
+    acc[e] *= inv;
+    const float x = __builtin_fabsf(acc[e]);
+    big = x < INFINITY ? fmaxf(big, x) : big;
+  }
+  const int ex = row_exp(wave_max(big));
+#pragma unroll
+  for (int e = 0; e < E; ++e) {
+    if (!on) break;
+    if constexpr (sizeof(T) == 2)
+      ((_Float16*)orow)[lane + 64 * e] = (_Float16)__builtin_amdgcn_ldexpf(acc[e], -ex);
+    else
+      ((float*)orow)[lane + 64 * e] = acc[e];
+  }
+  if (lane == 0) {
+    if constexpr (sizeof(T) == 2) encode_ml(m, l, ex, ml);
+    else *(float2*)ml = make_float2(l == 0.f ? -INFINITY : m, l);
+  }
+}
+
+// LDS of a work-group: the stage, or after the products the partial rows.
+template <class T, int D, int NT>
+struct TileLayout {
+  static constexpr int CPR = D * (int)sizeof(T) / 16, ROWS = 32 * NT;
+  static constexpr int VOFF = ROWS * CPR * 16, STAGE = 2 * VOFF;
+  static constexpr int OP = D * (int)sizeof(T) + 16, OUT = TROWS * OP;
+  static constexpr int BYTES = STAGE > OUT ? STAGE : OUT;
+};
+
+// 4 waves of 32 rows; NT 32-key tiles per stage.  Logits transposed, S^T = K Q^T,
+// so that the weights feed O^T += V^T P^T from their registers (in bf16 the
+// value operand comes from the rows of V by transposed LDS reads); a row of the
+// partial is one lane pair.  Consecutive tiles of a group go to one XCD.
+template <class T, int D, int NT, bool ONE>
+__global__ __launch_bounds__(256, D * sizeof(T) <= 128 ? 4 : D * sizeof(T) <= 256 ? 3 : 1) void k_block_tile(BlockAttendArgs p, BlockTileArgs w,
+                                                                                  BlockPartArgs part) {
+  using L = TileLayout<T, D, NT>;
+  constexpr bool BF = sizeof(T) == 2;
+  constexpr int CPR = L::CPR, NDT = D / 32, NQ = BF ? D / 16 : D / 8;
+  extern __shared__ __attribute__((aligned(1024))) uint8_t lds[];
+  const int64_t n_item = (int64_t)w.groups * w.tcap, per = (n_item + 7) / 8;
+  const int64_t it = (blockIdx.x & 7) * per + (blockIdx.x >> 3);
+  if (it >= n_item) return;
+  const int grp = (int)(it / w.tcap), tix = (int)(it - (int64_t)grp * w.tcap);
+  if (tix >= sload(w.ntiles + grp)) return;
+  const BlockTile* te = w.tiles + (int64_t)grp * w.tcap + tix;
+  const int b = sload(&te->b), rows = sload(&te->cnt) * p.G, row_a = sload(&te->part) * TROWS, start = sload(&te->start);
+  const int o = grp / p.H_kv, hk = grp - o * p.H_kv;
+  const int tid = threadIdx.x, lane = tid & 63, g = lane >> 5, l31 = lane & 31;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int64_t j0 = (int64_t)b * p.block;
+  const T* Kg = (const T*)p.K + o * p.ko + (int64_t)hk * D;
+  const T* Vg = (const T*)p.V + o * p.vo + (int64_t)hk * D;
+  // value rows: in bf16 four keys x 64 bytes per cycle, in fp32 two keys (4
+  // apart) x 128 bytes
+  auto fv = [](int r) { return BF ? Swz<CPR>::template v<CPR < 4 ? CPR : 4, 0>(r) : Swz<CPR>::template v<8, 2>(r); };
+  // Direct-to-LDS loads: load `it` of a wave covers 64 chunks, 256 / CPR rows
+  // after load it - 1; the swizzle repeats with every P loads, so that the lane's
+  // offsets are P numbers added to uniform addresses.  Rows past the last key
+  // read it again; no row sees them.
+  constexpr int NL = (L::ROWS * CPR + 255) / 256, P = CPR <= 16 ? 1 : CPR / 16, RPL = 256 / CPR;
+  const int c0 = wave * 64 + lane, r0 = c0 / CPR, x0 = c0 % CPR;
+  const int ksb = (int)p.ks * (int)sizeof(T), vsb = (int)p.vs * (int)sizeof(T);   // row strides below 2^24 bytes
+  int ko[P], vo[P];
+#pragma unroll
+  for (int i = 0; i < P; ++i) {
+    ko[i] = r0 * ksb + 16 * (x0 ^ Swz<CPR>::k(r0 + i * RPL));
+    vo[i] = r0 * vsb + 16 * (x0 ^ fv(r0 + i * RPL));
+  }
+  auto fill = [&](int st) {
+    const int64_t j = j0 + st * L::ROWS;
+    const uint8_t* kb = (const uint8_t*)(Kg + j * p.ks);
+    const uint8_t* vb = (const uint8_t*)(Vg + j * p.vs);
+    const int past = (int)max(j + L::ROWS - p.n_kv, (int64_t)0);   // rows of the stage that are not there
+    if (past == 0) {
+#pragma unroll
+      for (int i = 0; i < NL; ++i)
+        if (L::ROWS * CPR >= 256 * (i + 1) || wave * 64 < L::ROWS * CPR - 256 * i)
+          dma16(kb + (int64_t)i * RPL * ksb + ko[i % P], lds + (wave * 64 + 256 * i) * 16);
+#pragma unroll
+      for (int i = 0; i < NL; ++i)
+        if (L::ROWS * CPR >= 256 * (i + 1) || wave * 64 < L::ROWS * CPR - 256 * i)
+          dma16(vb + (int64_t)i * RPL * vsb + vo[i % P], lds + L::VOFF + (wave * 64 + 256 * i) * 16);
+    } else {
+      for (int i = 0; i < NL; ++i) {
+        if (wave * 64 >= L::ROWS * CPR - 256 * i) break;
+        const int r = r0 + i * RPL, up = max(r - max(L::ROWS - past - 1, 0), 0);   // rows back to the last key
+        const int64_t back = past >= L::ROWS ? r + 1 + (past - L::ROWS) : up;
+        dma16(kb + (r - back) * ksb + 16 * (x0 ^ Swz<CPR>::k(r)), lds + (wave * 64 + 256 * i) * 16);
+        dma16(vb + (r - back) * vsb + 16 * (x0 ^ fv(r)), lds + L::VOFF + (wave * 64 + 256 * i) * 16);
+      }
+    }
+  };
+  fill(0);
+  // this lane's row
+  const int row0 = row_a + wave * 32, row = min(row0 + l31, rows - 1), e = row / p.G, hg = row - e * p.G;
+  const uint32_t ent = gload(w.list + (int64_t)grp * w.nq * p.top_k + start + e);
+  const int i = (int)(ent / (uint32_t)p.top_k), slot = (int)(ent - (uint32_t)i * p.top_k);
+  const int64_t oi = (int64_t)o * p.n_q + w.i0 + i;
+  const int lim = (int)min((int64_t)visible_keys(p.n_vis, oi, p.n_kv) - j0, (int64_t)p.block);   // >= 1
+  const int prow = (((o * w.nq + i) * p.H_kv + hk) * p.top_k + slot) * p.G + hg;
+  const T* qp = (const T*)p.Q + o * p.qo + (w.i0 + i) * p.qs + (int64_t)(hk * p.G + hg) * D;
+  u32x4 q[NQ];
+#pragma unroll
+  for (int k = 0; k < NQ; ++k) q[k] = gload((const u32x4*)(qp + (BF ? 16 * k + 8 * g : 8 * k + 4 * g)));
+  f32x16 acc[NDT];
+  if constexpr (!ONE) {
+#pragma unroll
+    for (int dt = 0; dt < NDT; ++dt) acc[dt] = f32x16{};
+  }
+  float m = -INFINITY, l = 0.f;
+  const int n_st = ONE ? 1 : p.block / L::ROWS;
+  for (int st = 0; st < n_st; ++st) {
+    if (st > 0) {
+      stage_barrier();
+      fill(st);
+    }
+    wait_vmcnt<0>();
+    stage_barrier();
+    if (row0 >= rows) {   // (keeps the barriers)
+      if constexpr (ONE) break;
+      continue;
+    }
+    f32x16 sc[NT];
+#pragma unroll
+    for (int kt = 0; kt < NT; ++kt) {
+#pragma unroll
+      for (int k = 0; k < NQ; ++k) {
+        const u32x4 a = *(const u32x4*)(lds + ((32 * kt + l31) * CPR + ((2 * k + g) ^ Swz<CPR>::k(l31))) * 16);
+        if constexpr (BF) sc[kt] = mfma32(a, q[k], k == 0 ? f32x16{} : sc[kt]);
+        else sc[kt] = mfma32f(__builtin_bit_cast(f32x4, a), __builtin_bit_cast(f32x4, q[k]), k == 0 ? f32x16{} : sc[kt]);
+      }
+    }
+    const int left = lim - st * L::ROWS;
+    if (__any(left < L::ROWS)) {
+#pragma unroll
+      for (int kt = 0; kt < NT; ++kt)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) sc[kt][r] = 32 * kt + c_row(r, lane) < left ? sc[kt][r] : -INFINITY;
+    }
+    float mx = sc[0][0];
+#pragma unroll
+    for (int kt = 0; kt < NT; ++kt)
+#pragma unroll
+      for (int r = 0; r < 16; r += 2) mx = max3f(mx, sc[kt][r], sc[kt][r + 1]);
+    const float mn = __builtin_elementwise_maximum(m, max_with_partner(mx) * p.qscale);
+    const float sub = mn == -INFINITY ? 0.f : mn;
+    const float alpha = __builtin_amdgcn_exp2f(m - sub);
+    m = mn;
+    l *= alpha;
+    if (!ONE && st > 0) {
+#pragma unroll
+      for (int dt = 0; dt < NDT; ++dt) acc[dt] *= alpha;
+    }
+    if constexpr (BF) {
+      u32x4 pk[2 * NT];
+      float ts[2] = {0.f, 0.f};
+#pragma unroll
+      for (int ks = 0; ks < 2 * NT; ++ks)
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+          const float s0 = sc[ks >> 1][8 * (ks & 1) + 2 * x], s1 = sc[ks >> 1][8 * (ks & 1) + 2 * x + 1];
+          pk[ks][x] = pack_bf16x2(__builtin_amdgcn_exp2f(__builtin_fmaf(s0, p.qscale, -sub)),
+                                  __builtin_amdgcn_exp2f(__builtin_fmaf(s1, p.qscale, -sub)));
+          ts[ks & 1] = add_bf16x2(pk[ks][x], ts[ks & 1]);
+        }
+      l += ts[0] + ts[1];
+      const int kr = 4 * g + ((lane & 15) >> 2), f4 = fv(kr);   // the key row whose address this lane supplies
+      const uint8_t* vb = lds + L::VOFF + kr * CPR * 16 + (lane & 1) * 8;
+#pragma unroll
+      for (int dt = 0; dt < NDT; ++dt) {
+        const uint8_t* va = vb + ((4 * dt + 2 * ((lane >> 4) & 1) + ((lane >> 1) & 1)) ^ f4) * 16;
+#pragma unroll
+        for (int ks = 0; ks < 2 * NT; ++ks) {
+          const u32x2 lo = lds_tr4(va + 16 * ks * CPR * 16), hi = lds_tr4(va + (16 * ks + 8) * CPR * 16);
+          acc[dt] = mfma32(u32x4{lo[0], lo[1], hi[0], hi[1]}, pk[ks], ONE && ks == 0 ? f32x16{} : acc[dt]);
+        }
+      }
+    } else {
+#pragma unroll
+      for (int kt = 0; kt < NT; ++kt)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          sc[kt][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[kt][r], p.qscale, -sub));
+          l += sc[kt][r];
+        }
+#pragma unroll
+      for (int dt = 0; dt < NDT; ++dt)
+#pragma unroll
+        for (int kt = 0; kt < NT; ++kt)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) {
+            const int kr = 32 * kt + c_row(r, lane);
+            const float a = *(const float*)(lds + L::VOFF + (kr * CPR + ((8 * dt + (l31 >> 2)) ^ fv(kr))) * 16 + (l31 & 3) * 4);
+            acc[dt] = __builtin_amdgcn_mfma_f32_32x32x2f32(a, sc[kt][r], ONE && kt == 0 && r == 0 ? f32x16{} : acc[dt], 0, 0, 0);
+          }
+    }
+  }
+  stage_barrier();   // the stage is free
+  if (row0 >= rows) return;
+  l = sum_with_partner(l);
+  const float inv = l > 0.f ? __builtin_amdgcn_rcpf(l) : 0.f;
+  float big = 0.f;
+#pragma unroll
+  for (int dt = 0; dt < NDT; ++dt)
+#pragma unroll
+    for (int r = 0; r < 16; r += 2) big = max3f(big, __builtin_fabsf(acc[dt][r]), __builtin_fabsf(acc[dt][r + 1]));
+  big = max_with_partner(big);   // NaN if any value is
+  bool store = row0 + l31 < rows;
+  if (__any(!(big < INFINITY))) {
+    uint64_t todo = __ballot(store && g == 0 && !(big < INFINITY) && lim < p.block);
+    while (todo) {
+      const int r = __builtin_ctzll(todo);
+      todo &= todo - 1;
+      const int rrow = __builtin_amdgcn_readlane(prow, r), rlim = __builtin_amdgcn_readlane(lim, r);
+      const int ri = __builtin_amdgcn_readlane(i, r), rh = __builtin_amdgcn_readlane(hg, r);
+      careful_row<T, D>((const T*)p.Q + o * p.qo + (w.i0 + ri) * p.qs + (int64_t)(hk * p.G + rh) * D, Kg + j0 * p.ks,
+                        p.ks, Vg + j0 * p.vs, p.vs, rlim, p.qscale, (T*)part.Opart + (int64_t)rrow * D,
+                        part.ML + 2 * (int64_t)rrow);
+      store = store && l31 != r;
+    }
+    big = 0.f;
+#pragma unroll
+    for (int dt = 0; dt < NDT; ++dt)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const float x = __builtin_fabsf(acc[dt][r]);
+        big = x < INFINITY ? fmaxf(big, x) : big;
+      }
+    big = max_with_partner(big);
+  }
+  uint8_t* ow = lds + wave * 32 * L::OP;
+  if constexpr (BF) {
+    const int ex = row_exp(big * inv);
+    const float f = __builtin_amdgcn_ldexpf(inv, -ex);
+#pragma unroll
+    for (int dt = 0; dt < NDT; ++dt)
+#pragma unroll
+      for (int x = 0; x < 4; ++x) {
+        f16x4 v;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) v[r] = (_Float16)(acc[dt][4 * x + r] * f);
+        *(f16x4*)(ow + l31 * L::OP + (32 * dt + 8 * x + 4 * g) * 2) = v;
+      }
+    if (store && g == 0) encode_ml(m, l, ex, part.ML + 2 * (int64_t)prow);
+  } else {
+#pragma unroll
+    for (int dt = 0; dt < NDT; ++dt)
+#pragma unroll
+      for (int x = 0; x < 4; ++x)
+        *(f32x4*)(ow + l31 * L::OP + (32 * dt + 8 * x + 4 * g) * 4) =
+            f32x4{acc[dt][4 * x], acc[dt][4 * x + 1], acc[dt][4 * x + 2], acc[dt][4 * x + 3]} * inv;
+    if (store && g == 0) *(float2*)(part.ML + 2 * (int64_t)prow) = make_float2(l == 0.f ? -INFINITY : m, l);
+  }
+  // a wave's staged rows are written and read by that wave alone
+  __builtin_amdgcn_s_waitcnt(0xc07f);   // lgkmcnt(0)
+  __builtin_amdgcn_wave_barrier();
+  const uint32_t rows_ok = (uint32_t)__ballot(store);
+  constexpr int RPS = 64 / CPR < 1 ? 1 : 64 / CPR;   // rows of one store
+  const int rr0 = lane / CPR, xo = lane % CPR;
+  uint8_t* ob = (uint8_t*)part.Opart + 16 * xo;
+#pragma unroll
+  for (int k = 0; k < 32 / RPS; ++k) {
+    const int rr = rr0 + k * RPS;
+    const int pr = __shfl(prow, rr, 64);
+    const u32x4 val = *(const u32x4*)(ow + rr * L::OP + 16 * xo);
+    if ((rows_ok >> rr) & 1u) gstore((u32x4*)(ob + (uint64_t)(uint32_t)pr * (CPR * 16)), val);
+  }
+}
+
+template <class T, int D, int NT, bool ONE>
+hipError_t launch_stages(const BlockAttendArgs& a, const BlockTileArgs& t, const BlockPartArgs& w, hipStream_t st) {
+  const int64_t per = ((int64_t)t.groups * t.tcap + 7) / 8;
+  RS3_LAUNCH(RS3_K_BLOCK_ATTEND, st, (k_block_tile<T, D, NT, ONE>), dim3((unsigned)(8 * per)), dim3(256),
+             (TileLayout<T, D, NT>::BYTES), st, a, t, w);
+  return hipGetLastError();
+}
+
+template <class T, int D, int NT>
+hipError_t launch_tile(const BlockAttendArgs& a, const BlockTileArgs& t, const BlockPartArgs& w, hipStream_t st) {
+  return a.block == 32 * NT ? launch_stages<T, D, NT, true>(a, t, w, st) : launch_stages<T, D, NT, false>(a, t, w, st);
+}
+
+template <class T>
+hipError_t launch_width(const BlockAttendArgs& a, const BlockTileArgs& t, const BlockPartArgs& w, hipStream_t st) {
+  const bool one = a.block == 32;
+  switch (a.d_h) {
+    case 32: return one ? launch_tile<T, 32, 1>(a, t, w, st) : launch_tile<T, 32, 2>(a, t, w, st);
+    case 64: return one ? launch_tile<T, 64, 1>(a, t, w, st) : launch_tile<T, 64, 2>(a, t, w, st);
+    case 128: return one ? launch_tile<T, 128, 1>(a, t, w, st) : launch_tile<T, 128, 2>(a, t, w, st);
+    default:
+      if (one || sizeof(T) == 4) return launch_tile<T, 256, 1>(a, t, w, st);
+      if constexpr (sizeof(T) == 2) return launch_tile<T, 256, 2>(a, t, w, st);
+  }
+  return hipErrorInvalidValue;
+}
+
+}  // namespace rs3
+
+using namespace rs3;
+
+hipError_t rs3_launch_block_tile(const BlockAttendArgs& a, const BlockTileArgs& t, const BlockPartArgs& w, int dtype,
+                                 hipStream_t st) {
+  const dim3 grid(t.runs, t.groups);
+  RS3_LAUNCH(RS3_K_BLOCK_ATTEND, st, k_block_count, grid, dim3(512), a.n_blk * 4, st, a, t, w);
+  RS3_LAUNCH(RS3_K_BLOCK_ATTEND, st, k_block_scatter, grid, dim3(512), a.n_blk * 8, st, a, t);
+  return dtype == RS3_BF16 ? launch_width<bf16_t>(a, t, w, st) : launch_width<float>(a, t, w, st);
+}
+
+template <class T, int D, int NT>
+static hipError_t allow() {
+  const hipError_t e = hipFuncSetAttribute((const void*)k_block_tile<T, D, NT, true>,
+                                           hipFuncAttributeMaxDynamicSharedMemorySize, TileLayout<T, D, NT>::BYTES);
+  return e != hipSuccess ? e
+                         : hipFuncSetAttribute((const void*)k_block_tile<T, D, NT, false>,
+                                               hipFuncAttributeMaxDynamicSharedMemorySize, TileLayout<T, D, NT>::BYTES);
+}
+
+hipError_t rs3_block_tile_setup() {
+  const hipError_t es[] = {
+      hipFuncSetAttribute((const void*)k_block_scatter, hipFuncAttributeMaxDynamicSharedMemorySize, BLOCK_TILE_MAX * 8),
+      allow<bf16_t, 128, 1>(), allow<bf16_t, 128, 2>(), allow<bf16_t, 256, 1>(), allow<bf16_t, 256, 2>(),
+      allow<float, 64, 2>(), allow<float, 128, 1>(), allow<float, 128, 2>(), allow<float, 256, 1>()};
+  for (hipError_t e : es)
+    if (e != hipSuccess) return e;
+  return hipSuccess;
+}

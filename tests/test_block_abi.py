@@ -77,7 +77,7 @@ def test_every_call_refuses_the_shape(p, kw):
     (dict(k_stride=120), ("means", "attend")), (dict(k_stride=132), ("means", "attend")),
     (dict(k_obj_stride=-128), ("means", "attend")), (dict(v_stride=64), ("attend",)), (dict(q_stride=248), ("select", "attend")),
     (dict(q_obj_stride=4), ("select", "attend")), (dict(o_stride=8), ("attend",)), (dict(o_obj_stride=0), ("attend",)),
-    (dict(o_obj_stride=256), ("attend",)), (dict(k_stride=1 << 40), ("means", "attend"))])
+    (dict(o_obj_stride=256), ("attend",)), (dict(k_stride=1 << 40), ("means", "attend")), (dict(v_stride=1 << 22), ("attend",))])
 def test_row_layouts_refused(p, kw, who):
     s = shape(p, **kw)
     # only the calls that must refuse are made: the others would launch
