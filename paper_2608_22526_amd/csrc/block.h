@@ -53,25 +53,30 @@ struct BlockAttendArgs {
 
 // Blocks of keys that the counters of the tiled attention hold.
 constexpr int BLOCK_TILE_MAX = 8192;
+// Waves of a work-group of the tiled attention, 32 (query, head) rows each.
+constexpr int BLOCK_TILE_WAVES = 4;
 
-// Workspace of the tiled attention for one run of queries (i0 .. i0 + nq of
-// every object); a group is an (object, key head) pair.
+// Workspace of the tiled attention.  A group is an (object, key head) pair; the
+// queries of every object are taken `chunk` at a time, so that the partial rows
+// of a chunk are still in the memory-side cache when they are merged.
 struct BlockTile {
-  int b, part;             // block, and which 128 of its (query, head) rows
-  int start, cnt;          // the block's queries in the group's list
+  int b, n;                // block (-1: no tile), and how many queries
 };
 struct BlockTileArgs {
-  uint32_t* ord;           // [groups][nq][top_k] place of an entry among its run's queries of that block, ~0: none
-  uint32_t* hist;          // [runs][groups][n_blk] queries of each run that list the block
-  uint32_t* list;          // [groups][nq * top_k] query * top_k + slot, by block
-  BlockTile* tiles;        // [groups][tcap]
-  int32_t* ntiles;         // [groups]
-  int i0, nq, tcap, groups, runs, run;   // run: queries of one counting work-group
+  uint32_t* ord;           // [groups][n_q][top_k] place of an entry among its run's queries of its block,
+                           //   times BLOCK_TILE_MAX, + the block; ~0: none
+  uint32_t* total;         // [chunks][groups][n_blk] queries that list the block
+  uint32_t* base;          // [chunks * runs][groups][n_blk] where each run's begin among them
+  uint32_t* list;          // [chunks][groups][tcap][tq] query of the chunk * top_k + slot
+  BlockTile* tiles;        // [chunks][groups][tcap]
+  int chunk, chunks, ch, nq;   // queries per chunk, chunks; this launch's chunk and its queries
+  int run, runs;           // queries of one counting work-group, runs per chunk
+  int tq, tcap, groups;    // queries of a tile at most, tiles of a group and chunk at most
 };
 
-// Partial rows, merged by k_block_merge: row ((o * nq + i) * H_kv + g) * S + s)
-// * G + head of [d_h] values and (m, l) pairs; s is a slot of the list (tiled
-// form) or a split of the keys.
+// Partial rows, merged by k_block_merge: O row (((o * nq + i) * H_kv + g) * S + s)
+// * G + head of a chunk's nq queries, (m, l) pair of the same row among all n_q;
+// s is a slot of the list (tiled form) or a split of the keys.
 struct BlockPartArgs {
   void* Opart;
   float* ML;
@@ -123,6 +128,8 @@ hipError_t rs3_launch_qk_norm(const rs3::QkNormArgs& a, int dtype, hipStream_t s
 hipError_t rs3_launch_block_means(const rs3::BlockMeansArgs& a, int n_obj, int dtype, hipStream_t st);
 hipError_t rs3_launch_block_select(const rs3::BlockSelectArgs& a, int dtype, hipStream_t st);
 hipError_t rs3_launch_block_row(const rs3::BlockAttendArgs& a, const rs3::BlockPartArgs& w, int dtype, hipStream_t st);
+hipError_t rs3_launch_block_lists(const rs3::BlockAttendArgs& a, const rs3::BlockTileArgs& t,
+                                  const rs3::BlockPartArgs& w, hipStream_t st);
 hipError_t rs3_launch_block_tile(const rs3::BlockAttendArgs& a, const rs3::BlockTileArgs& t,
                                  const rs3::BlockPartArgs& w, int dtype, hipStream_t st);
 hipError_t rs3_launch_block_merge(const rs3::BlockAttendArgs& a, const rs3::BlockPartArgs& w, int dtype, bool f16,

@@ -57,14 +57,13 @@ size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
 
 // How a call of rs3_block_attend runs.
 struct AttendPlan {
-  bool tile;         // tiled form, in runs of `step` queries of every object
-  int step, S;       // S: splits of a row's keys (other form)
-  int groups, runs, run, tcap;
-  size_t ord, hist, list, tiles, ntiles, opart, ml, total;
+  bool tile;         // tiled form
+  int S;             // splits of a row's keys (other form)
+  int groups, chunk, chunks, run, runs, tq, tcap;
+  size_t ord, cnt, base, list, tiles, opart, ml, total;
 };
 
-constexpr int TROWS = 128;   // of block_tile.hip
-constexpr size_t PART_BYTES = (size_t)640 << 20;   // partial rows of one run of queries
+constexpr size_t PART_BYTES = (size_t)256 << 20;   // partial rows of a chunk of queries
 
 void attend_plan(const rs3_block_shape* s, AttendPlan* a) {
   memset(a, 0, sizeof(*a));
@@ -75,31 +74,30 @@ void attend_plan(const rs3_block_shape* s, AttendPlan* a) {
     off += align256(bytes);
     return at;
   };
-  a->tile = s->n_q >= 64 && n_blk <= BLOCK_TILE_MAX && n_blk > 0;
+  const size_t per_q = (size_t)s->n_obj * s->H * s->top_k * s->d_h * elem(s->dt);   // partial rows of one query
+  a->tile = s->n_q >= 64 && n_blk <= BLOCK_TILE_MAX && n_blk > 0 && per_q <= (16u << 20) && G <= 32 * BLOCK_TILE_WAVES;
   if (a->tile) {
-    const size_t per_q = (size_t)s->n_obj * s->H * s->top_k * (s->d_h * elem(s->dt) + 8);
-    const int64_t most_q = std::max<int64_t>(512, (int64_t)(PART_BYTES / per_q)), parts = (s->n_q + most_q - 1) / most_q;
-    a->step = (int)((s->n_q + parts - 1) / parts);
+    const int64_t most_q = std::min<int64_t>(1 << 20, std::max<int64_t>(64, (int64_t)(PART_BYTES / per_q)));
+    a->chunks = (int)((s->n_q + most_q - 1) / most_q);
+    a->chunk = (s->n_q + a->chunks - 1) / a->chunks;
     a->groups = s->n_obj * s->H_kv;
-    // every scattering work-group adds up the counts of all runs
-    int most = 65536 / n_blk;
-    most = most < 4 ? 4 : most > 64 ? 64 : most;
-    a->run = (a->step + most - 1) / most;
+    a->run = 2048 / s->top_k;
     if (a->run < 64) a->run = 64;
-    a->runs = (a->step + a->run - 1) / a->run;
-    const int64_t entries = (int64_t)a->step * s->top_k;
-    a->tcap = (int)(entries * G / TROWS + (n_blk < entries ? n_blk : entries));
-    a->ord = take(entries * a->groups * 4);
-    a->hist = take((size_t)a->runs * a->groups * n_blk * 4);
-    a->list = take(entries * a->groups * 4);
-    a->tiles = take((size_t)a->tcap * a->groups * sizeof(BlockTile));
-    a->ntiles = take((size_t)a->groups * 4);
+    a->runs = (a->chunk + a->run - 1) / a->run;
+    a->tq = 32 * BLOCK_TILE_WAVES / G;
+    const int64_t entries = (int64_t)a->chunk * s->top_k;
+    a->tcap = (int)(entries / a->tq + (n_blk < entries ? n_blk : entries));
+    a->ord = take((size_t)s->n_q * s->top_k * a->groups * 4);
+    a->cnt = take((size_t)a->chunks * a->groups * n_blk * 4);
+    a->base = take((size_t)a->chunks * a->runs * a->groups * n_blk * 4);
+    a->list = take((size_t)a->chunks * a->tcap * a->groups * a->tq * 4);
+    a->tiles = take((size_t)a->chunks * a->tcap * a->groups * sizeof(BlockTile));
     a->opart = take(entries * s->H * s->n_obj * s->d_h * elem(s->dt));
-    a->ml = take(entries * s->H * s->n_obj * 8);
+    a->ml = take((size_t)s->n_q * s->top_k * s->H * s->n_obj * 8);
   } else {
-    // work-groups for the chip twice over, each with a few pieces of 32 keys per wave
+    // a work-group per CU, each with a few pieces of 32 keys per wave
     const int64_t rows = (int64_t)s->n_obj * s->n_q * s->H_kv * ((G + 15) / 16);
-    int64_t S = rows > 0 ? 512 / rows : 1;
+    int64_t S = rows > 0 ? 256 / rows : 1;
     const int64_t most = (int64_t)s->top_k * s->block / 32 / 8;
     S = S < most ? S : most;
     a->S = (int)(S < 1 ? 1 : S);
@@ -304,19 +302,22 @@ rs3_status rs3_block_attend(const rs3_block_shape* s, const void* Q, const void*
   BlockTileArgs t;
   memset(&t, 0, sizeof(t));
   t.ord = (uint32_t*)(w + pl.ord);
-  t.hist = (uint32_t*)(w + pl.hist);
+  t.total = (uint32_t*)(w + pl.cnt);
+  t.base = (uint32_t*)(w + pl.base);
   t.list = (uint32_t*)(w + pl.list);
   t.tiles = (BlockTile*)(w + pl.tiles);
-  t.ntiles = (int32_t*)(w + pl.ntiles);
+  t.chunk = pl.chunk;
+  t.chunks = pl.chunks;
   t.run = pl.run;
+  t.runs = pl.runs;
+  t.tq = pl.tq;
   t.tcap = pl.tcap;
   t.groups = pl.groups;
   part.S = s->top_k;
-  hipError_t e = hipSuccess;
-  for (int i0 = 0; i0 < s->n_q && e == hipSuccess; i0 += pl.step) {
-    part.i0 = t.i0 = i0;
-    part.nq = t.nq = s->n_q - i0 < pl.step ? s->n_q - i0 : pl.step;
-    t.runs = (t.nq + pl.run - 1) / pl.run;
+  hipError_t e = rs3_launch_block_lists(a, t, part, st);
+  for (t.ch = 0; t.ch < pl.chunks && e == hipSuccess; ++t.ch) {
+    part.i0 = t.ch * pl.chunk;
+    part.nq = t.nq = std::min(pl.chunk, s->n_q - part.i0);
     e = rs3_launch_block_tile(a, t, part, s->dt, st);
     if (e == hipSuccess) e = rs3_launch_block_merge(a, part, s->dt, true, st);
   }

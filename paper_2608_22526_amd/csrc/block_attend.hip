@@ -269,6 +269,7 @@ __global__ __launch_bounds__(256) void k_block_merge(BlockAttendArgs p, BlockPar
   const int64_t o = oq / w.nq, i = oq - o * w.nq;
   if (o >= p.n_obj) return;
   const int64_t row0 = (oq * p.H_kv + hk) * w.S * p.G + (h - hk * p.G);
+  const int64_t ml0 = ((o * p.n_q + w.i0 + i) * p.H_kv + hk) * w.S * p.G + (h - hk * p.G);
   float M = -INFINITY, W = 0.f, acc[CH];
 #pragma unroll
   for (int e = 0; e < CH; ++e) acc[e] = 0.f;
@@ -279,14 +280,14 @@ __global__ __launch_bounds__(256) void k_block_merge(BlockAttendArgs p, BlockPar
     float top = M;
 #pragma unroll
     for (int k = 0; k < NB; ++k) {
-      const int64_t row = row0 + (int64_t)min(s0 + k, w.S - 1) * p.G;
-      const u32x2 ml = gload((const u32x2*)(w.ML + 2 * row));
+      const int64_t at = (int64_t)min(s0 + k, w.S - 1) * p.G, row = row0 + at;
+      const u32x2 ml = gload((const u32x2*)(w.ML + 2 * (ml0 + at)));
       m[k] = s0 + k < w.S ? __uint_as_float(ml[0]) : -INFINITY;
       l[k] = __uint_as_float(ml[1]);
 #pragma unroll
       for (int x = 0; x < (F16 ? 1 : CH / 4); ++x)
-        v[k][x] = F16 ? gload((const u32x4*)((const bf16_t*)w.Opart + row * p.d_h + d0))
-                      : gload((const u32x4*)((const float*)w.Opart + row * p.d_h + d0) + x);
+        v[k][x] = F16 ? pload((const u32x4*)((const bf16_t*)w.Opart + row * p.d_h + d0))
+                      : pload((const u32x4*)((const float*)w.Opart + row * p.d_h + d0) + x);
     }
 #pragma unroll
     for (int k = 0; k < NB; ++k) top = fmaxf(top, m[k]);

@@ -17,104 +17,125 @@ namespace rs3 {
 
 typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
 
-constexpr int TROWS = 128;  // rows of a tile, 32 per wave
 
-// grid (runs, groups), 512 threads, n_blk counters in LDS.  Entries that take
-// no part (out of range, not ascending, past the count, not seen) get no place
-// and an empty partial.
+// The blocks' counters to 0 (a kernel, which a graph can hold).
+__global__ __launch_bounds__(256) void k_block_zero(uint32_t* total, int64_t n) {
+  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (i < n) total[i] = 0;
+}
+
+// grid (runs of all chunks, groups), 512 threads, n_blk counters in LDS.  Entries
+// that take no part (out of range, not ascending, past the count, not seen) get
+// no place and an empty partial.
 __global__ __launch_bounds__(512) void k_block_count(BlockAttendArgs p, BlockTileArgs w, BlockPartArgs part) {
   extern __shared__ uint32_t sc[];
-  const int run = blockIdx.x, grp = blockIdx.y, o = grp / p.H_kv, hk = grp - o * p.H_kv, tid = threadIdx.x;
+  const int grp = blockIdx.y, o = grp / p.H_kv, hk = grp - o * p.H_kv, tid = threadIdx.x;
+  const int ch = blockIdx.x / w.runs, q0 = ch * w.chunk + (blockIdx.x - ch * w.runs) * w.run;
+  const int items = max(min(w.run, min((ch + 1) * w.chunk, p.n_q) - q0), 0) * p.top_k;
   for (int b = tid; b < p.n_blk; b += 512) sc[b] = 0;
   __syncthreads();
-  const int q0 = run * w.run, items = min(w.run, w.nq - q0) * p.top_k;
   for (int e = tid; e < items; e += 512) {
-    const int iq = e / p.top_k, t = e - iq * p.top_k, i = q0 + iq;
-    const int64_t oi = (int64_t)o * p.n_q + w.i0 + i, row = oi * p.H_kv + hk;
+    const int iq = e / p.top_k, t = e - iq * p.top_k;
+    const int64_t oi = (int64_t)o * p.n_q + q0 + iq, row = oi * p.H_kv + hk;
     const int32_t* list = p.idx + row * p.top_k;
     const int b = gload(list + t), prev = gload(list + max(t - 1, 0)), cnt = min(gload(p.count + row), p.top_k);
     const bool ok = t < cnt && b >= 0 && b < p.n_blk && (t == 0 || b > prev) &&
                     (int64_t)b * p.block < visible_keys(p.n_vis, oi, p.n_kv);
     uint32_t at = ~0u;
     if (ok) {
-      at = atomicAdd(&sc[b], 1u);
+      at = atomicAdd(&sc[b], 1u) * BLOCK_TILE_MAX + (uint32_t)b;
     } else {
-      float* ml = part.ML + (((((int64_t)o * w.nq + i) * p.H_kv + hk) * p.top_k + t) * p.G) * 2;
+      float* ml = part.ML + (row * p.top_k + t) * p.G * 2;
       for (int g = 0; g < p.G; ++g) {
         ml[2 * g] = -INFINITY;
         ml[2 * g + 1] = 0.f;
       }
     }
-    w.ord[((int64_t)grp * w.nq + i) * p.top_k + t] = at;
+    w.ord[((int64_t)grp * p.n_q + q0) * p.top_k + e] = at;
   }
   __syncthreads();
-  for (int b = tid; b < p.n_blk; b += 512) w.hist[((int64_t)run * w.groups + grp) * p.n_blk + b] = sc[b];
+  // the run's place among the chunk's: in the order in which the runs come by,
+  // which decides where a row is computed and nothing else
+  uint32_t* total = w.total + ((int64_t)ch * w.groups + grp) * p.n_blk;
+  uint32_t* base = w.base + ((int64_t)blockIdx.x * w.groups + grp) * p.n_blk;
+  for (int b = tid; b < p.n_blk; b += 512)
+    if (sc[b]) base[b] = atomicAdd(total + b, sc[b]);
 }
 
-// Same grid: every work-group adds up the runs' counts of its group (they are
-// few), so that no launch has to hand them on; run 0 writes the tiles.  LDS:
-// the blocks' counts and then where this run's queries of each begin.
+// Same grid: the run's entries into the lists; each chunk's first run writes the
+// tiles.  LDS: where this run's queries of each block begin, the blocks' counts
+// and first tiles.
 __global__ __launch_bounds__(512) void k_block_scatter(BlockAttendArgs p, BlockTileArgs w) {
   extern __shared__ uint32_t sm[];
-  __shared__ uint64_t wsum[8];
+  __shared__ uint32_t wsum[8], ntile;
   uint32_t* pre = sm;
   uint32_t* tot = sm + p.n_blk;
-  const int run = blockIdx.x, grp = blockIdx.y, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int ch = blockIdx.x / w.runs, run = blockIdx.x - ch * w.runs, grp = blockIdx.y;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int64_t cg = (int64_t)ch * w.groups + grp;
   for (int b = tid; b < p.n_blk; b += 512) {
-    uint32_t a = 0, t = 0;
-    for (int r0 = 0; r0 < w.runs; r0 += 8) {
-      uint32_t n[8];
-#pragma unroll
-      for (int k = 0; k < 8; ++k)
-        n[k] = gload(w.hist + ((int64_t)min(r0 + k, w.runs - 1) * w.groups + grp) * p.n_blk + b);
-#pragma unroll
-      for (int k = 0; k < 8; ++k) {
-        a += r0 + k < run ? n[k] : 0;
-        t += r0 + k < w.runs ? n[k] : 0;
-      }
-    }
-    pre[b] = a;
-    tot[b] = t;
+    tot[b] = gload(w.total + cg * p.n_blk + b);
+    pre[b] = gload(w.base + ((int64_t)blockIdx.x * w.groups + grp) * p.n_blk + b);   // (anything, where it has none)
   }
+  const int q0 = ch * w.chunk + run * w.run;
+  const int items = max(min(w.run, min((ch + 1) * w.chunk, p.n_q) - q0), 0) * p.top_k;
+  const uint32_t* ord = w.ord + ((int64_t)grp * p.n_q + q0) * p.top_k;
+  uint32_t at4[4];   // in flight during the scan
+#pragma unroll
+  for (int k = 0; k < 4; ++k) at4[k] = tid + 512 * k < items ? gload(ord + tid + 512 * k) : ~0u;
   __syncthreads();
-  // exclusive scan over the blocks of (entries << 32 | tiles), a stretch of blocks per thread
+  // exclusive scan of the blocks' tiles, a stretch of blocks per thread; a tile's
+  // queries begin at tq times its number in the list
+  const uint32_t tq = w.tq;
   const int per = (p.n_blk + 511) / 512, b0 = min(tid * per, p.n_blk), b1 = min(b0 + per, p.n_blk);
-  uint64_t mine = 0;
-  for (int b = b0; b < b1; ++b) mine += ((uint64_t)tot[b] << 32) | ((tot[b] * (uint32_t)p.G + TROWS - 1) / TROWS);
-  uint64_t incl = mine;
+  uint32_t mine = 0;
+  for (int b = b0; b < b1; ++b) mine += (tot[b] + tq - 1) / tq;
+  uint32_t incl = mine;
   for (int d = 1; d < 64; d <<= 1) {
-    const uint64_t up = __shfl_up(incl, d, 64);
+    const uint32_t up = __shfl_up(incl, d, 64);
     if (lane >= d) incl += up;
   }
   if (lane == 63) wsum[wave] = incl;
   __syncthreads();
-  uint64_t at = incl - mine;
+  uint32_t at = incl - mine;
   for (int i = 0; i < wave; ++i) at += wsum[i];
-  BlockTile* tiles = w.tiles + (int64_t)grp * w.tcap;
+  if (tid == 511) ntile = at + mine;
+  uint32_t* first = sm + 2 * p.n_blk;   // first tile of each block
   for (int b = b0; b < b1; ++b) {
-    const uint32_t n = tot[b], start = (uint32_t)(at >> 32), nt = (n * (uint32_t)p.G + TROWS - 1) / TROWS;
-    pre[b] += start;
-    if (run == 0)
-      for (uint32_t t = 0; t < nt; ++t) {
-        BlockTile e;
-        e.b = b;
-        e.part = (int)t;
-        e.start = (int)start;
-        e.cnt = (int)n;
-        tiles[(uint32_t)at + t] = e;
-      }
-    at += ((uint64_t)n << 32) | nt;
+    first[b] = at;
+    pre[b] += at * tq;
+    at += (tot[b] + tq - 1) / tq;
   }
-  if (run == 0 && tid == 511) w.ntiles[grp] = (int)(uint32_t)at;
   __syncthreads();
-  const int q0 = run * w.run, items = min(w.run, w.nq - q0) * p.top_k, o = grp / p.H_kv, hk = grp - o * p.H_kv;
-  const int64_t base = (int64_t)grp * w.nq * p.top_k;
-  for (int e = tid; e < items; e += 512) {
-    const uint32_t place = gload(w.ord + base + (int64_t)q0 * p.top_k + e);
-    if (place == ~0u) continue;
-    const int iq = e / p.top_k, t = e - iq * p.top_k;
-    const int64_t row = ((int64_t)o * p.n_q + w.i0 + q0 + iq) * p.H_kv + hk;
-    w.list[base + pre[gload(p.idx + row * p.top_k + t)] + place] = (uint32_t)(q0 * p.top_k + e);
+  if (run == 0) {
+    BlockTile* tiles = w.tiles + cg * w.tcap;
+    for (uint32_t t = tid; t < (uint32_t)w.tcap; t += 512) {
+      BlockTile e;
+      e.b = -1;
+      e.n = 0;
+      if (t < ntile) {   // its block: the last whose first tile is not past t
+        int lo = 0, hi = p.n_blk;
+        while (hi - lo > 1) {
+          const int mid = (lo + hi) >> 1;
+          if (first[mid] <= t) lo = mid;
+          else hi = mid;
+        }
+        e.b = lo;
+        e.n = (int)min(tot[lo] - (t - first[lo]) * tq, tq);
+      }
+      tiles[t] = e;
+    }
+  }
+  uint32_t* list = w.list + cg * w.tcap * tq;
+  for (int e0 = tid; e0 < items; e0 += 2048) {
+    if (e0 > tid) {
+#pragma unroll
+      for (int k = 0; k < 4; ++k) at4[k] = e0 + 512 * k < items ? gload(ord + e0 + 512 * k) : ~0u;
+    }
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+      if (at4[k] != ~0u)
+        list[pre[at4[k] % BLOCK_TILE_MAX] + at4[k] / BLOCK_TILE_MAX] = (uint32_t)(run * w.run * p.top_k + e0 + 512 * k);
   }
 }
 
@@ -191,47 +212,56 @@ __device__ __noinline__ void careful_row(const T* q, const T* k, int64_t ks, con
   }
 }
 
-// LDS of a work-group: the stage, or after the products the partial rows.
-template <class T, int D, int NT>
+// LDS of a work-group: the stage, and after the products for each wave 32 rows
+// of a segment of its partial rows (128 bytes, or the whole of a 64-byte row).
+template <class T, int D, int NT, int NW>
 struct TileLayout {
   static constexpr int CPR = D * (int)sizeof(T) / 16, ROWS = 32 * NT;
   static constexpr int VOFF = ROWS * CPR * 16, STAGE = 2 * VOFF;
-  static constexpr int OP = D * (int)sizeof(T) + 16, OUT = TROWS * OP;
+  static constexpr int SEG = CPR < 8 ? CPR : 8;   // chunks of a segment
+  static constexpr int OUT = NW * 32 * SEG * 16;
   static constexpr int BYTES = STAGE > OUT ? STAGE : OUT;
+  // chunk c of row r lies at chunk c ^ f(r): 16 rows at one chunk, or whole rows, per LDS cycle
+  static __device__ __forceinline__ int f(int r) { return (r / (16 / SEG)) & (SEG - 1); }
 };
 
-// 4 waves of 32 rows; NT 32-key tiles per stage.  Logits transposed, S^T = K Q^T,
-// so that the weights feed O^T += V^T P^T from their registers (in bf16 the
-// value operand comes from the rows of V by transposed LDS reads); a row of the
-// partial is one lane pair.  Consecutive tiles of a group go to one XCD.
-template <class T, int D, int NT, bool ONE>
-__global__ __launch_bounds__(256, D * sizeof(T) <= 128 ? 4 : D * sizeof(T) <= 256 ? 3 : 1) void k_block_tile(BlockAttendArgs p, BlockTileArgs w,
-                                                                                  BlockPartArgs part) {
-  using L = TileLayout<T, D, NT>;
+// NW waves of 32 rows; NT 32-key tiles per stage; ONE: the block is one stage.
+// Logits transposed, S^T = K Q^T, so that the weights feed O^T += V^T P^T from
+// their registers (in bf16 the value operand comes from the rows of V by
+// transposed LDS reads); a row of the partial is one lane pair.  Consecutive
+// tiles of a group go to one XCD.
+template <class T, int D, int NT, int NW, bool ONE>
+__global__ __launch_bounds__(64 * NW, D * sizeof(T) <= 256 ? (D * sizeof(T) <= 128 || ONE ? 4 : 3) : 1) void k_block_tile(
+    BlockAttendArgs p, BlockTileArgs w, BlockPartArgs part) {
+  using L = TileLayout<T, D, NT, NW>;
   constexpr bool BF = sizeof(T) == 2;
-  constexpr int CPR = L::CPR, NDT = D / 32, NQ = BF ? D / 16 : D / 8;
+  constexpr int CPR = L::CPR, NDT = D / 32, NQ = BF ? D / 16 : D / 8, TH = 64 * NW;
   extern __shared__ __attribute__((aligned(1024))) uint8_t lds[];
   const int64_t n_item = (int64_t)w.groups * w.tcap, per = (n_item + 7) / 8;
   const int64_t it = (blockIdx.x & 7) * per + (blockIdx.x >> 3);
   if (it >= n_item) return;
-  const int grp = (int)(it / w.tcap), tix = (int)(it - (int64_t)grp * w.tcap);
-  if (tix >= sload(w.ntiles + grp)) return;
-  const BlockTile* te = w.tiles + (int64_t)grp * w.tcap + tix;
-  const int b = sload(&te->b), rows = sload(&te->cnt) * p.G, row_a = sload(&te->part) * TROWS, start = sload(&te->start);
+  const int grp = (int)(it / w.tcap);
+  const int64_t tile = (int64_t)w.ch * n_item + it;
+  const int b = sload(&w.tiles[tile].b), rows = sload(&w.tiles[tile].n) * p.G;
   const int o = grp / p.H_kv, hk = grp - o * p.H_kv;
   const int tid = threadIdx.x, lane = tid & 63, g = lane >> 5, l31 = lane & 31;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  // this lane's row: list entry, then query, keys seen, partial row
+  const int row0 = wave * 32;
+  const uint32_t lrow = (uint32_t)(row0 + l31), e = min(lrow / (uint32_t)p.G, (uint32_t)w.tq - 1);
+  uint32_t ent = gload(w.list + tile * w.tq + e);   // (read beside the tile: a place without a query holds anything)
+  if (b < 0) return;
   const int64_t j0 = (int64_t)b * p.block;
   const T* Kg = (const T*)p.K + o * p.ko + (int64_t)hk * D;
   const T* Vg = (const T*)p.V + o * p.vo + (int64_t)hk * D;
   // value rows: in bf16 four keys x 64 bytes per cycle, in fp32 two keys (4
   // apart) x 128 bytes
   auto fv = [](int r) { return BF ? Swz<CPR>::template v<CPR < 4 ? CPR : 4, 0>(r) : Swz<CPR>::template v<8, 2>(r); };
-  // Direct-to-LDS loads: load `it` of a wave covers 64 chunks, 256 / CPR rows
-  // after load it - 1; the swizzle repeats with every P loads, so that the lane's
+  // Direct-to-LDS loads: load i of a wave covers 64 chunks, RPL rows after load
+  // i - 1; the swizzle repeats with every P loads, so that the lane's
   // offsets are P numbers added to uniform addresses.  Rows past the last key
   // read it again; no row sees them.
-  constexpr int NL = (L::ROWS * CPR + 255) / 256, P = CPR <= 16 ? 1 : CPR / 16, RPL = 256 / CPR;
+  constexpr int NL = (L::ROWS * CPR + TH - 1) / TH, RPL = TH / CPR, P = RPL >= 16 ? 1 : 16 / RPL;
   const int c0 = wave * 64 + lane, r0 = c0 / CPR, x0 = c0 % CPR;
   const int ksb = (int)p.ks * (int)sizeof(T), vsb = (int)p.vs * (int)sizeof(T);   // row strides below 2^24 bytes
   int ko[P], vo[P];
@@ -248,31 +278,34 @@ __global__ __launch_bounds__(256, D * sizeof(T) <= 128 ? 4 : D * sizeof(T) <= 25
     if (past == 0) {
 #pragma unroll
       for (int i = 0; i < NL; ++i)
-        if (L::ROWS * CPR >= 256 * (i + 1) || wave * 64 < L::ROWS * CPR - 256 * i)
-          dma16(kb + (int64_t)i * RPL * ksb + ko[i % P], lds + (wave * 64 + 256 * i) * 16);
+        if (L::ROWS * CPR >= TH * (i + 1) || wave * 64 < L::ROWS * CPR - TH * i)
+          dma16(kb + (int64_t)i * RPL * ksb + ko[i % P], lds + (wave * 64 + TH * i) * 16);
 #pragma unroll
       for (int i = 0; i < NL; ++i)
-        if (L::ROWS * CPR >= 256 * (i + 1) || wave * 64 < L::ROWS * CPR - 256 * i)
-          dma16(vb + (int64_t)i * RPL * vsb + vo[i % P], lds + L::VOFF + (wave * 64 + 256 * i) * 16);
+        if (L::ROWS * CPR >= TH * (i + 1) || wave * 64 < L::ROWS * CPR - TH * i)
+          dma16(vb + (int64_t)i * RPL * vsb + vo[i % P], lds + L::VOFF + (wave * 64 + TH * i) * 16);
     } else {
       for (int i = 0; i < NL; ++i) {
-        if (wave * 64 >= L::ROWS * CPR - 256 * i) break;
+        if (wave * 64 >= L::ROWS * CPR - TH * i) break;
         const int r = r0 + i * RPL, up = max(r - max(L::ROWS - past - 1, 0), 0);   // rows back to the last key
         const int64_t back = past >= L::ROWS ? r + 1 + (past - L::ROWS) : up;
-        dma16(kb + (r - back) * ksb + 16 * (x0 ^ Swz<CPR>::k(r)), lds + (wave * 64 + 256 * i) * 16);
-        dma16(vb + (r - back) * vsb + 16 * (x0 ^ fv(r)), lds + L::VOFF + (wave * 64 + 256 * i) * 16);
+        dma16(kb + (r - back) * ksb + 16 * (x0 ^ Swz<CPR>::k(r)), lds + (wave * 64 + TH * i) * 16);
+        dma16(vb + (r - back) * vsb + 16 * (x0 ^ fv(r)), lds + L::VOFF + (wave * 64 + TH * i) * 16);
       }
     }
   };
   fill(0);
-  // this lane's row
-  const int row0 = row_a + wave * 32, row = min(row0 + l31, rows - 1), e = row / p.G, hg = row - e * p.G;
-  const uint32_t ent = gload(w.list + (int64_t)grp * w.nq * p.top_k + start + e);
-  const int i = (int)(ent / (uint32_t)p.top_k), slot = (int)(ent - (uint32_t)i * p.top_k);
-  const int64_t oi = (int64_t)o * p.n_q + w.i0 + i;
-  const int lim = (int)min((int64_t)visible_keys(p.n_vis, oi, p.n_kv) - j0, (int64_t)p.block);   // >= 1
-  const int prow = (((o * w.nq + i) * p.H_kv + hk) * p.top_k + slot) * p.G + hg;
-  const T* qp = (const T*)p.Q + o * p.qo + (w.i0 + i) * p.qs + (int64_t)(hk * p.G + hg) * D;
+  const int i0 = w.ch * w.chunk;
+  const bool there = row0 + l31 < rows;
+  ent = there ? ent : 0;
+  const int hg = there ? (int)(lrow - e * (uint32_t)p.G) : 0;
+  const int qi = (int)(ent / (uint32_t)p.top_k), slot = (int)(ent - (uint32_t)qi * p.top_k);
+  const int64_t oi = (int64_t)o * p.n_q + i0 + qi;
+  const int lim = (int)min((int64_t)visible_keys(p.n_vis, oi, p.n_kv) - j0, (int64_t)p.block);
+  const int prow = (((o * w.nq + qi) * p.H_kv + hk) * p.top_k + slot) * p.G + hg;
+  float* ml = part.ML + 2 * (((oi * p.H_kv + hk) * p.top_k + slot) * p.G + hg);
+  const T* Qo = (const T*)p.Q + o * p.qo + (int64_t)i0 * p.qs + (int64_t)hk * p.G * D;
+  const T* qp = Qo + qi * p.qs + hg * D;
   u32x4 q[NQ];
 #pragma unroll
   for (int k = 0; k < NQ; ++k) q[k] = gload((const u32x4*)(qp + (BF ? 16 * k + 8 * g : 8 * k + 4 * g)));
@@ -284,16 +317,13 @@ __global__ __launch_bounds__(256, D * sizeof(T) <= 128 ? 4 : D * sizeof(T) <= 25
   float m = -INFINITY, l = 0.f;
   const int n_st = ONE ? 1 : p.block / L::ROWS;
   for (int st = 0; st < n_st; ++st) {
-    if (st > 0) {
+    if (!ONE && st > 0) {
       stage_barrier();
       fill(st);
     }
     wait_vmcnt<0>();
     stage_barrier();
-    if (row0 >= rows) {   // (keeps the barriers)
-      if constexpr (ONE) break;
-      continue;
-    }
+    if (row0 >= rows) continue;
     f32x16 sc[NT];
 #pragma unroll
     for (int kt = 0; kt < NT; ++kt) {
@@ -379,17 +409,19 @@ __global__ __launch_bounds__(256, D * sizeof(T) <= 128 ? 4 : D * sizeof(T) <= 25
 #pragma unroll
     for (int r = 0; r < 16; r += 2) big = max3f(big, __builtin_fabsf(acc[dt][r]), __builtin_fabsf(acc[dt][r + 1]));
   big = max_with_partner(big);   // NaN if any value is
-  bool store = row0 + l31 < rows;
+  bool store = there;
   if (__any(!(big < INFINITY))) {
     uint64_t todo = __ballot(store && g == 0 && !(big < INFINITY) && lim < p.block);
     while (todo) {
       const int r = __builtin_ctzll(todo);
       todo &= todo - 1;
       const int rrow = __builtin_amdgcn_readlane(prow, r), rlim = __builtin_amdgcn_readlane(lim, r);
-      const int ri = __builtin_amdgcn_readlane(i, r), rh = __builtin_amdgcn_readlane(hg, r);
-      careful_row<T, D>((const T*)p.Q + o * p.qo + (w.i0 + ri) * p.qs + (int64_t)(hk * p.G + rh) * D, Kg + j0 * p.ks,
-                        p.ks, Vg + j0 * p.vs, p.vs, rlim, p.qscale, (T*)part.Opart + (int64_t)rrow * D,
-                        part.ML + 2 * (int64_t)rrow);
+      const int ri = __builtin_amdgcn_readlane(qi, r), rh = __builtin_amdgcn_readlane(hg, r);
+      const uint64_t at = (uint64_t)(uintptr_t)ml;
+      const uint64_t rml = (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(at >> 32), r) << 32 |
+                           (uint32_t)__builtin_amdgcn_readlane((int)at, r);
+      careful_row<T, D>(Qo + ri * p.qs + rh * D, Kg + j0 * p.ks, p.ks, Vg + j0 * p.vs, p.vs, rlim, p.qscale,
+                        (T*)part.Opart + (int64_t)rrow * D, (float*)rml);
       store = store && l31 != r;
     }
     big = 0.f;
@@ -402,50 +434,72 @@ __global__ __launch_bounds__(256, D * sizeof(T) <= 128 ? 4 : D * sizeof(T) <= 25
       }
     big = max_with_partner(big);
   }
-  uint8_t* ow = lds + wave * 32 * L::OP;
+  float f = inv;
   if constexpr (BF) {
     const int ex = row_exp(big * inv);
-    const float f = __builtin_amdgcn_ldexpf(inv, -ex);
+    f = __builtin_amdgcn_ldexpf(inv, -ex);
+    if (store && g == 0) encode_ml(m, l, ex, ml);
+  } else {
+    if (store && g == 0) *(float2*)ml = make_float2(l == 0.f ? -INFINITY : m, l);
+  }
+  uint8_t* ow = lds + wave * 32 * L::SEG * 16;
+  const uint32_t rows_ok = (uint32_t)__ballot(store);
+  // a segment of the rows at a time through the wave's own LDS, then whole segments in 16-byte stores
+  constexpr int RPS = 64 / L::SEG, RN = 32 / RPS;   // rows of a store
+  const int rr0 = lane / L::SEG, xo = lane % L::SEG;
+  uint8_t* ob = (uint8_t*)part.Opart + 16 * xo;
+  uint64_t oo[RN];
 #pragma unroll
-    for (int dt = 0; dt < NDT; ++dt)
+  for (int k = 0; k < RN; ++k) oo[k] = (uint64_t)(uint32_t)__shfl(prow, rr0 + k * RPS, 64) * (CPR * 16);
+#pragma unroll
+  for (int sg = 0; sg < CPR / L::SEG; ++sg) {
+    if constexpr (BF) {
+      constexpr int DTS = L::SEG / 4;   // 32-channel blocks of a segment
+#pragma unroll
+      for (int d = 0; d < DTS; ++d)
+#pragma unroll
+        for (int x = 0; x < 4; x += 2) {
+          const f32x16& a = acc[sg * DTS + d];
+          auto pk2 = [&](int i) {
+            typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+            const f16x2 v = {(_Float16)(a[i] * f), (_Float16)(a[i + 1] * f)};
+            return __builtin_bit_cast(uint32_t, v);
+          };
+          // channels 8x .. 8x+3 (+4 g) and 8x+8 .. +11 (+4 g): the lane pair swaps halves,
+          // so that each lane holds eight neighbours
+          const auto s0 = __builtin_amdgcn_permlane32_swap(pk2(4 * x), pk2(4 * x + 4), false, false);
+          const auto s1 = __builtin_amdgcn_permlane32_swap(pk2(4 * x + 2), pk2(4 * x + 6), false, false);
+          *(u32x4*)(ow + (l31 * L::SEG + ((4 * d + x + g) ^ L::f(l31))) * 16) = u32x4{s0[0], s1[0], s0[1], s1[1]};
+        }
+    } else {
 #pragma unroll
       for (int x = 0; x < 4; ++x) {
-        f16x4 v;
-#pragma unroll
-        for (int r = 0; r < 4; ++r) v[r] = (_Float16)(acc[dt][4 * x + r] * f);
-        *(f16x4*)(ow + l31 * L::OP + (32 * dt + 8 * x + 4 * g) * 2) = v;
+        const f32x16& a = acc[sg];
+        *(f32x4*)(ow + (l31 * L::SEG + ((2 * x + g) ^ L::f(l31))) * 16) =
+            f32x4{a[4 * x], a[4 * x + 1], a[4 * x + 2], a[4 * x + 3]} * f;
       }
-    if (store && g == 0) encode_ml(m, l, ex, part.ML + 2 * (int64_t)prow);
-  } else {
+    }
+    __builtin_amdgcn_s_waitcnt(0xc07f);   // lgkmcnt(0)
+    __builtin_amdgcn_wave_barrier();
+    u32x4 val[RN];
 #pragma unroll
-    for (int dt = 0; dt < NDT; ++dt)
+    for (int k = 0; k < RN; ++k) {
+      const int rr = rr0 + k * RPS;
+      val[k] = *(const u32x4*)(ow + (rr * L::SEG + (xo ^ L::f(rr))) * 16);
+    }
 #pragma unroll
-      for (int x = 0; x < 4; ++x)
-        *(f32x4*)(ow + l31 * L::OP + (32 * dt + 8 * x + 4 * g) * 4) =
-            f32x4{acc[dt][4 * x], acc[dt][4 * x + 1], acc[dt][4 * x + 2], acc[dt][4 * x + 3]} * inv;
-    if (store && g == 0) *(float2*)(part.ML + 2 * (int64_t)prow) = make_float2(l == 0.f ? -INFINITY : m, l);
-  }
-  // a wave's staged rows are written and read by that wave alone
-  __builtin_amdgcn_s_waitcnt(0xc07f);   // lgkmcnt(0)
-  __builtin_amdgcn_wave_barrier();
-  const uint32_t rows_ok = (uint32_t)__ballot(store);
-  constexpr int RPS = 64 / CPR < 1 ? 1 : 64 / CPR;   // rows of one store
-  const int rr0 = lane / CPR, xo = lane % CPR;
-  uint8_t* ob = (uint8_t*)part.Opart + 16 * xo;
-#pragma unroll
-  for (int k = 0; k < 32 / RPS; ++k) {
-    const int rr = rr0 + k * RPS;
-    const int pr = __shfl(prow, rr, 64);
-    const u32x4 val = *(const u32x4*)(ow + rr * L::OP + 16 * xo);
-    if ((rows_ok >> rr) & 1u) gstore((u32x4*)(ob + (uint64_t)(uint32_t)pr * (CPR * 16)), val);
+    for (int k = 0; k < RN; ++k)
+      if ((rows_ok >> (rr0 + k * RPS)) & 1u) pstore((u32x4*)(ob + oo[k] + sg * L::SEG * 16), val[k]);
+    __builtin_amdgcn_wave_barrier();
   }
 }
 
 template <class T, int D, int NT, bool ONE>
 hipError_t launch_stages(const BlockAttendArgs& a, const BlockTileArgs& t, const BlockPartArgs& w, hipStream_t st) {
+  constexpr int NW = BLOCK_TILE_WAVES;
   const int64_t per = ((int64_t)t.groups * t.tcap + 7) / 8;
-  RS3_LAUNCH(RS3_K_BLOCK_ATTEND, st, (k_block_tile<T, D, NT, ONE>), dim3((unsigned)(8 * per)), dim3(256),
-             (TileLayout<T, D, NT>::BYTES), st, a, t, w);
+  RS3_LAUNCH(RS3_K_BLOCK_ATTEND, st, (k_block_tile<T, D, NT, NW, ONE>), dim3((unsigned)(8 * per)), dim3(64 * NW),
+             (TileLayout<T, D, NT, NW>::BYTES), st, a, t, w);
   return hipGetLastError();
 }
 
@@ -472,26 +526,32 @@ hipError_t launch_width(const BlockAttendArgs& a, const BlockTileArgs& t, const 
 
 using namespace rs3;
 
+hipError_t rs3_launch_block_lists(const BlockAttendArgs& a, const BlockTileArgs& t, const BlockPartArgs& w,
+                                  hipStream_t st) {
+  const dim3 grid(t.runs * t.chunks, t.groups);
+  const int64_t n = (int64_t)t.chunks * t.groups * a.n_blk;
+  RS3_LAUNCH(RS3_K_BLOCK_ATTEND, st, k_block_zero, dim3((unsigned)((n + 255) / 256)), dim3(256), 0, st, t.total, n);
+  RS3_LAUNCH(RS3_K_BLOCK_ATTEND, st, k_block_count, grid, dim3(512), a.n_blk * 4, st, a, t, w);
+  RS3_LAUNCH(RS3_K_BLOCK_ATTEND, st, k_block_scatter, grid, dim3(512), a.n_blk * 12, st, a, t);
+  return hipGetLastError();
+}
+
 hipError_t rs3_launch_block_tile(const BlockAttendArgs& a, const BlockTileArgs& t, const BlockPartArgs& w, int dtype,
                                  hipStream_t st) {
-  const dim3 grid(t.runs, t.groups);
-  RS3_LAUNCH(RS3_K_BLOCK_ATTEND, st, k_block_count, grid, dim3(512), a.n_blk * 4, st, a, t, w);
-  RS3_LAUNCH(RS3_K_BLOCK_ATTEND, st, k_block_scatter, grid, dim3(512), a.n_blk * 8, st, a, t);
   return dtype == RS3_BF16 ? launch_width<bf16_t>(a, t, w, st) : launch_width<float>(a, t, w, st);
 }
 
 template <class T, int D, int NT>
 static hipError_t allow() {
-  const hipError_t e = hipFuncSetAttribute((const void*)k_block_tile<T, D, NT, true>,
-                                           hipFuncAttributeMaxDynamicSharedMemorySize, TileLayout<T, D, NT>::BYTES);
-  return e != hipSuccess ? e
-                         : hipFuncSetAttribute((const void*)k_block_tile<T, D, NT, false>,
-                                               hipFuncAttributeMaxDynamicSharedMemorySize, TileLayout<T, D, NT>::BYTES);
+  constexpr int NW = BLOCK_TILE_WAVES, bytes = TileLayout<T, D, NT, NW>::BYTES;
+  const hipFuncAttribute at = hipFuncAttributeMaxDynamicSharedMemorySize;
+  const hipError_t e = hipFuncSetAttribute((const void*)k_block_tile<T, D, NT, NW, true>, at, bytes);
+  return e != hipSuccess ? e : hipFuncSetAttribute((const void*)k_block_tile<T, D, NT, NW, false>, at, bytes);
 }
 
 hipError_t rs3_block_tile_setup() {
   const hipError_t es[] = {
-      hipFuncSetAttribute((const void*)k_block_scatter, hipFuncAttributeMaxDynamicSharedMemorySize, BLOCK_TILE_MAX * 8),
+      hipFuncSetAttribute((const void*)k_block_scatter, hipFuncAttributeMaxDynamicSharedMemorySize, BLOCK_TILE_MAX * 12),
       allow<bf16_t, 128, 1>(), allow<bf16_t, 128, 2>(), allow<bf16_t, 256, 1>(), allow<bf16_t, 256, 2>(),
       allow<float, 64, 2>(), allow<float, 128, 1>(), allow<float, 128, 2>(), allow<float, 256, 1>()};
   for (hipError_t e : es)
