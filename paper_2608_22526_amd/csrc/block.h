@@ -33,9 +33,18 @@ struct BlockSelectArgs {
   const int32_t* n_vis;    // [n_obj][n_q] or null
   int32_t* idx;            // [n_obj][n_q][H_kv][top_k]
   int32_t* count;          // [n_obj][n_q][H_kv]
-  double* score;           // [rows][n_blk] workspace
+  double* score;           // [rows][n_blk] workspace, or null
   int64_t rows;            // n_obj * n_q * H_kv
   int n_obj, n_q, n_kv, H, H_kv, d_h, block, n_blk, top_k, n_first, n_last;
+};
+
+// How a call of rs3_block_select runs.
+constexpr int SELECT_LDS = 131072;   // at most
+struct BlockSelectPlan {
+  bool tile;         // several queries of a key head per work-group, else one
+  int TR, pitch;     // tile: queries, floats of a row of scores
+  int split;         // else: work-groups that share a row's blocks, whose scores go to the workspace (1: LDS)
+  int lds;
 };
 
 struct BlockAttendArgs {
@@ -126,7 +135,9 @@ __device__ __forceinline__ T from_f32(float v) {
 
 hipError_t rs3_launch_qk_norm(const rs3::QkNormArgs& a, int dtype, hipStream_t st);
 hipError_t rs3_launch_block_means(const rs3::BlockMeansArgs& a, int n_obj, int dtype, hipStream_t st);
-hipError_t rs3_launch_block_select(const rs3::BlockSelectArgs& a, int dtype, hipStream_t st);
+hipError_t rs3_launch_block_select(const rs3::BlockSelectArgs& a, const rs3::BlockSelectPlan& pl, int dtype,
+                                   hipStream_t st);
+hipError_t rs3_block_select_setup();
 hipError_t rs3_launch_block_row(const rs3::BlockAttendArgs& a, const rs3::BlockPartArgs& w, int dtype, hipStream_t st);
 hipError_t rs3_launch_block_lists(const rs3::BlockAttendArgs& a, const rs3::BlockTileArgs& t,
                                   const rs3::BlockPartArgs& w, hipStream_t st);

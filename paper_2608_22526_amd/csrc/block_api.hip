@@ -118,8 +118,34 @@ rs3_status ensure_setup() {
   return RS3_OK;
 }
 
-size_t select_ws(const rs3_block_shape* s) {
-  return (size_t)s->n_obj * s->n_q * s->H_kv * n_blocks(s) * sizeof(double);
+void select_plan(const rs3_block_shape* s, BlockSelectPlan* a, size_t* ws) {
+  memset(a, 0, sizeof(*a));
+  *ws = 0;
+  const int64_t n_blk = n_blocks(s), rows = (int64_t)s->n_obj * s->n_q * s->H_kv;
+  a->split = 1;
+  // Several queries: the largest tile whose scores leave room for two work-groups
+  // per CU, at least four queries.
+  const int q_lds = 2 * 32 * s->d_h * 2;   // the queries' two terms
+  a->pitch = (int)((n_blk + 31) / 32 * 32 + 4);
+  if (s->n_q >= 8) {
+    int TR = 32;
+    while (TR > 4 && (TR * a->pitch * 4 > 81920 - 2048 || TR / 2 >= s->n_q)) TR /= 2;
+    int64_t lds = (int64_t)TR * a->pitch * 4;
+    lds = std::max<int64_t>(lds, std::max<int64_t>(n_blk * 8, q_lds));
+    if (lds <= SELECT_LDS) {
+      a->tile = true;
+      a->TR = TR;
+      a->lds = (int)lds;
+      return;
+    }
+  }
+  // One query per work-group: its blocks over several where there are few rows
+  // or the scores do not fit the LDS.
+  int64_t split = rows > 0 && rows < 128 ? std::min<int64_t>(256 / rows, n_blk / 128) : 1;
+  if (n_blk * 8 > SELECT_LDS) split = std::max<int64_t>(split, (n_blk + 4095) / 4096);
+  a->split = (int)(split < 1 ? 1 : split);
+  if (a->split > 1) *ws = (size_t)rows * n_blk * sizeof(double);
+  else a->lds = (int)std::max<int64_t>(n_blk * 8, 16);
 }
 
 }  // namespace
@@ -198,7 +224,8 @@ rs3_status rs3_block_means(const rs3_block_shape* s, const void* K, const int32_
 
 rs3_status rs3_block_select_workspace_size(const rs3_block_shape* s, size_t* bytes) {
   if (!bytes || !shape_ok(s)) return RS3_E_INVALID;
-  *bytes = select_ws(s);
+  BlockSelectPlan pl;
+  select_plan(s, &pl, bytes);
   return RS3_OK;
 }
 
@@ -208,8 +235,12 @@ rs3_status rs3_block_select(const rs3_block_shape* s, const void* Q, const void*
   if (!aligned16(Q) || !aligned16(Kmean) || !aligned16(ws)) return RS3_E_INVALID;
   if (s->n_q == 0) return RS3_OK;
   if (!Q || !idx || !count || (s->n_kv > 0 && !Kmean)) return RS3_E_INVALID;
-  const size_t need = select_ws(s);
+  BlockSelectPlan pl;
+  size_t need;
+  select_plan(s, &pl, &need);
   if (need > 0 && (!ws || ws_bytes < need)) return RS3_E_INVALID;
+  const rs3_status st0 = ensure_setup();
+  if (st0 != RS3_OK) return st0;
   BlockSelectArgs a;
   memset(&a, 0, sizeof(a));
   a.Q = Q;
@@ -232,7 +263,7 @@ rs3_status rs3_block_select(const rs3_block_shape* s, const void* Q, const void*
   a.top_k = s->top_k;
   a.n_first = s->n_first;
   a.n_last = s->n_last;
-  return map_err(rs3_launch_block_select(a, s->dt, (hipStream_t)stream));
+  return map_err(rs3_launch_block_select(a, pl, s->dt, (hipStream_t)stream));
 }
 
 rs3_status rs3_block_attend_workspace_size(const rs3_block_shape* s, size_t* bytes) {

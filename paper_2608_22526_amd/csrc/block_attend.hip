@@ -370,7 +370,7 @@ hipError_t rs3_launch_block_merge(const BlockAttendArgs& a, const BlockPartArgs&
 hipError_t rs3_block_setup() {
   const hipError_t es[] = {allow<bf16_t, 32>(), allow<bf16_t, 64>(), allow<bf16_t, 128>(), allow<bf16_t, 256>(),
                            allow<float, 32>(), allow<float, 64>(), allow<float, 128>(), allow<float, 256>(),
-                           rs3_block_tile_setup()};
+                           rs3_block_tile_setup(), rs3_block_select_setup()};
   for (hipError_t e : es)
     if (e != hipSuccess) return e;
   return hipSuccess;
