@@ -17,7 +17,8 @@
 
 namespace rs3 {
 
-constexpr int NWS = 8;        // waves of a work-group
+constexpr int NWS = 8;        // waves of a work-group of k_select_tile
+constexpr int NWR = 16;       // of k_select_row: more of the mean keys in flight per CU
 constexpr int VPL = 8;        // scores that a lane keeps in registers
 
 // Order of the scores as unsigned integers; a NaN counts as -inf.  0 is no score.
@@ -29,25 +30,22 @@ __device__ __forceinline__ uint64_t key64(double s) {
 __device__ __forceinline__ double of_key64(uint64_t k) {
   return __longlong_as_double((long long)(k >> 63 ? k ^ (1ull << 63) : ~k));
 }
-__device__ __forceinline__ uint32_t key32(float s) {
-  if (s != s) s = -INFINITY;
-  const uint32_t u = __float_as_uint(s == 0.f ? 0.f : s);
-  return u >> 31 ? ~u : u | (1u << 31);
-}
-__device__ __forceinline__ float of_key32(uint32_t k) { return __uint_as_float(k >> 31 ? k ^ (1u << 31) : ~k); }
 
 // The blocks of one row: of those it sees [0, nb), [0, f_lo) and [last0, nb) are
 // forced and `want` of the others are to be found.
 struct RowRange {
   int nb, f_lo, last0, want;
 };
-__device__ __forceinline__ RowRange row_range(const BlockSelectArgs& p, int64_t oi) {
+__device__ __forceinline__ RowRange range_of(const BlockSelectArgs& p, int nb) {
   RowRange r;
-  r.nb = (visible_keys(p.n_vis, oi, p.n_kv) + p.block - 1) / p.block;
+  r.nb = nb;
   r.last0 = max(r.nb - p.n_last, 0);
   r.f_lo = min(p.n_first, r.last0);
   r.want = min(p.top_k, r.nb) - (r.f_lo + r.nb - r.last0);
   return r;
+}
+__device__ __forceinline__ RowRange row_range(const BlockSelectArgs& p, int64_t oi) {
+  return range_of(p, (visible_keys(p.n_vis, oi, p.n_kv) + p.block - 1) / p.block);
 }
 
 __device__ __forceinline__ double wave_sum64(double v) {
@@ -56,111 +54,152 @@ __device__ __forceinline__ double wave_sum64(double v) {
   return v;
 }
 
-// The list of one row from its fp64 scores, by the whole work-group: the largest
-// key that `want` scores reach, by halving (first of the values, which needs few
-// steps for ordinary scores, then of the keys, which always ends), then the
-// blocks above it and the lowest of those at it.  A wave owns a stretch of
-// blocks.  sh: 3 * NWS words of LDS.
-__device__ void pick_row(const double* sc, const RowRange& r, int top_k, int32_t* idx, int32_t* count, int* sh) {
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int seg = (r.nb + 64 * NWS - 1) / (64 * NWS), b0 = wave * seg * 64;
+// Minimum and maximum over the lanes by the exchanges of wave_max.
+__device__ __forceinline__ float wave_min(float v) { return -wave_max(-v); }
+
+// Bits of the 64 blocks from 64 j on that lie in [a, b).
+__device__ __forceinline__ uint64_t range_bits(int j, int a, int b) {
+  const int lo = min(max(a - 64 * j, 0), 64), hi = min(max(b - 64 * j, 0), 64);
+  if (lo >= hi) return 0;
+  return (~0ull >> (64 - (hi - lo))) << lo;
+}
+__device__ __forceinline__ uint64_t forced_bits(const RowRange& r, int j) {
+  if (64 * j >= r.f_lo && 64 * j + 64 <= r.last0) return 0;
+  return range_bits(j, 0, r.f_lo) | range_bits(j, r.last0, r.nb);
+}
+
+// LDS of pick_row: three counters in turn, and a word or two per wave.
+template <int NW>
+struct PickLds {
+  unsigned long long n[3];
+  float f[2 * NW];
+};
+
+// The list of one row from its fp64 scores, by a work-group of NW waves: the
+// largest key that `want` scores reach, by quartering (first of the values, which
+// needs few steps for ordinary scores, then of the keys, which always ends),
+// then the blocks above it and the lowest of those at it.  A wave owns a stretch
+// of blocks.
+template <int NW>
+__device__ void pick_row(const double* sc, const RowRange& r, int top_k, int32_t* idx, int32_t* count, PickLds<NW>& sh) {
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int seg = (r.nb + 64 * NW - 1) / (64 * NW), j0 = wave * seg;
   const uint64_t below = (1ull << lane) - 1;
   auto key_at = [&](int j) -> uint64_t {
-    const int b = b0 + 64 * j + lane;
+    const int b = 64 * (j0 + j) + lane;
     return b >= r.f_lo && b < r.last0 ? key64(sc[b]) : 0ull;
   };
   uint64_t kept[VPL];
 #pragma unroll
   for (int j = 0; j < VPL; ++j) kept[j] = j < seg ? key_at(j) : 0ull;
-  int turn = 0;
-  auto reach = [&](uint64_t t) {   // scores at or above t, over the work-group
-    int n = 0;
+  // scores at or above t[0..2], over the work-group: 21 bits of a counter each
+  int slot = 0;
+  if (tid < 3) sh.n[tid] = 0;
+  auto reach = [&](const uint64_t (&t)[3], int (&n)[3]) {
+    n[0] = n[1] = n[2] = 0;
 #pragma unroll
-    for (int j = 0; j < VPL; ++j) n += (int)__popcll(__ballot(kept[j] >= t));
-    for (int j = VPL; j < seg; ++j) n += (int)__popcll(__ballot(key_at(j) >= t));
-    if (lane == 0) sh[turn * NWS + wave] = n;
+    for (int j = 0; j < VPL; ++j)
+      if (j < seg)
+#pragma unroll
+        for (int x = 0; x < 3; ++x) n[x] += (int)__popcll(__ballot(kept[j] >= t[x]));
+    for (int j = VPL; j < seg; ++j) {
+      const uint64_t k = key_at(j);
+#pragma unroll
+      for (int x = 0; x < 3; ++x) n[x] += (int)__popcll(__ballot(k >= t[x]));
+    }
+    if (lane == 0)
+      atomicAdd(&sh.n[slot], (unsigned long long)n[0] | (unsigned long long)n[1] << 21 | (unsigned long long)n[2] << 42);
     __syncthreads();
-    n = 0;
+    const unsigned long long all = sh.n[slot];
+    // the counter of the step before last: everybody has read it
+    if (tid == 0) sh.n[slot == 0 ? 2 : slot - 1] = 0;
+    slot = slot == 2 ? 0 : slot + 1;
 #pragma unroll
-    for (int w = 0; w < NWS; ++w) n += sh[turn * NWS + w];
-    turn ^= 1;
-    return n;
+    for (int x = 0; x < 3; ++x) n[x] = (int)(all >> (21 * x)) & 0x1fffff;
   };
   uint64_t lo = 1, hi = ~0ull;   // `want` scores reach lo, fewer reach hi
   int above = 0;
   if (r.want > 0) {
-    double span = 0.0;   // the largest finite magnitude, as a start
+    // ordinary scores: the largest finite one, and the smallest of the lanes' largest
+    float top = -INFINITY, low;
 #pragma unroll
     for (int j = 0; j < VPL; ++j) {
-      const double x = kept[j] ? fabs(of_key64(kept[j])) : 0.0;
-      span = x < INFINITY ? fmax(span, x) : span;
+      const float x = kept[j] ? (float)of_key64(kept[j]) : -INFINITY;
+      top = x < INFINITY ? fmaxf(top, x) : top;
     }
-    float top = (float)span;
+    low = wave_min(top == -INFINITY ? INFINITY : top);
     top = wave_max(top);
-    if (lane == 0) sh[2 * NWS + wave] = __float_as_int(top);
+    if (lane == 0) {
+      sh.f[wave] = top;
+      sh.f[NW + wave] = low;
+    }
     __syncthreads();
-    top = 0.f;
-#pragma unroll
-    for (int w = 0; w < NWS; ++w) top = fmaxf(top, __int_as_float(sh[2 * NWS + w]));
-    double vlo = -2.0 * top, vhi = 2.0 * top;
+    top = wave_max(sh.f[lane % NW]);
+    low = wave_min(sh.f[NW + lane % NW]);
+    const double room = 1e-3 * ((double)top - low) + 1e-6 * fabs(top);
+    double vlo = low - room, vhi = top + room;
     bool found = false;
-    for (int step = 0; step < 20 && top > 0.f && top < INFINITY; ++step) {
-      const double v = 0.5 * (vlo + vhi);
-      const uint64_t t = key64(v);
-      if (!(t > lo && t < hi)) break;
-      const int n = reach(t);
-      if (n >= r.want) {
-        lo = t;
-        vlo = v;
-      } else {
-        hi = t;
-        vhi = v;
-      }
-      if (n == r.want) {
-        found = true;
-        break;
-      }
+    uint64_t t[3];
+    int n[3];
+    for (int step = 0; step < 12 && fabs(vlo) < INFINITY && fabs(vhi) < INFINITY; ++step) {
+      const double d = 0.25 * (vhi - vlo);
+#pragma unroll
+      for (int x = 0; x < 3; ++x) t[x] = key64(vlo + d * (x + 1));
+      if (!(t[0] > lo && t[2] < hi && t[0] < t[1] && t[1] < t[2])) break;
+      reach(t, n);
+      const int at = (n[0] >= r.want) + (n[1] >= r.want) + (n[2] >= r.want);
+      if (at > 0) lo = at == 1 ? t[0] : at == 2 ? t[1] : t[2];
+      if (at < 3) hi = at == 0 ? t[0] : at == 1 ? t[1] : t[2];
+      found = at > 0 && (at == 1 ? n[0] : at == 2 ? n[1] : n[2]) == r.want;
+      if (found) break;
+      const double base = vlo;
+      if (at > 0) vlo = base + d * at;
+      if (at < 3) vhi = base + d * (at + 1);
     }
     while (!found && hi - lo > 1) {
-      const uint64_t t = lo + ((hi - lo) >> 1);
-      const int n = reach(t);
-      if (n >= r.want) lo = t;
-      else hi = t;
-      found = n == r.want;
+      const uint64_t q = (hi - lo) >> 2, h = (hi - lo) >> 1;
+      t[0] = lo + (q ? q : 1);
+      t[1] = lo + h;
+      t[2] = hi - (q ? q : 1);
+      reach(t, n);
+      const int at = (n[0] >= r.want) + (n[1] >= r.want) + (n[2] >= r.want);
+      if (at > 0) lo = at == 1 ? t[0] : at == 2 ? t[1] : t[2];
+      if (at < 3) hi = at == 0 ? t[0] : at == 1 ? t[1] : t[2];
+      found = at > 0 && (at == 1 ? n[0] : at == 2 ? n[1] : n[2]) == r.want;
     }
-    above = reach(lo + 1);
+    t[0] = t[1] = t[2] = lo + 1;
+    reach(t, n);
+    above = n[0];
   }
   // kept: forced, above lo, and the first want - above at lo
   int n_eq = 0, n_keep = 0;
   for (int j = 0; j < seg; ++j) {
-    const int b = b0 + 64 * j + lane;
     const uint64_t k = r.want > 0 ? key_at(j) : 0ull;
     n_eq += (int)__popcll(__ballot(k == lo));
-    n_keep += (int)__popcll(__ballot((b < r.nb && (b < r.f_lo || b >= r.last0)) || k > lo));
+    n_keep += (int)__popcll(__ballot(k > lo) | forced_bits(r, j0 + j));
   }
   __syncthreads();
   if (lane == 0) {
-    sh[wave] = n_eq;
-    sh[NWS + wave] = n_keep;
+    sh.f[wave] = (float)n_eq;
+    sh.f[NW + wave] = (float)n_keep;
   }
   __syncthreads();
-  int ties = r.want - above, out = 0;   // ties left to this wave, entries before it
-  for (int w = 0; w < wave; ++w) {
-    out += sh[NWS + w] + min(max(ties, 0), sh[w]);
-    ties -= sh[w];
-  }
+  // entries of the waves before this one
+  const int eq_before = (int)wave_sum(lane < wave ? sh.f[lane % NW] : 0.f);
+  const int keep_before = (int)wave_sum(lane < wave ? sh.f[NW + lane % NW] : 0.f);
+  int ties = r.want - above, out = keep_before + min(max(ties, 0), eq_before);
+  ties -= eq_before;
   for (int j = 0; j < seg; ++j) {
-    const int b = b0 + 64 * j + lane;
     const uint64_t k = r.want > 0 ? key_at(j) : 0ull;
-    const uint64_t eq = __ballot(k == lo);
-    const bool keep = (b < r.nb && (b < r.f_lo || b >= r.last0)) || k > lo || (k == lo && (int)__popcll(eq & below) < ties);
+    const uint64_t eq = __ballot(k == lo), at_lo = __ballot(k == lo && (int)__popcll(eq & below) < ties);
     ties -= (int)__popcll(eq);
-    const uint64_t m = __ballot(keep);
-    if (keep) idx[out + (int)__popcll(m & below)] = b;
+    const uint64_t m = __ballot(k > lo) | forced_bits(r, j0 + j) | at_lo;
+    const int at = out + (int)__popcll(m & below);
+    if ((m >> lane & 1) && at < top_k) idx[at] = 64 * (j0 + j) + lane;
     out += (int)__popcll(m);
   }
   const int n_all = min(top_k, r.nb);
-  for (int t = n_all + tid; t < top_k; t += 64 * NWS) idx[t] = -1;
+  for (int t = n_all + tid; t < top_k; t += 64 * NW) idx[t] = -1;
   if (tid == 0) *count = n_all;
 }
 
@@ -175,9 +214,9 @@ __device__ __forceinline__ float chunk_val(const u32x4& v, int e) {
 // block, each with EPL channels of the query summed over its heads (products of
 // finite values stay in the fp64 range; where a score is infinite or no number
 // the products are added up head by head, whose infinities the sum could hide).
-template <class T, int D>
+template <class T, int D, int NW>
 __device__ void score_row(const BlockSelectArgs& p, const T* q, const T* km, int a, int b, double* sc) {
-  constexpr int EPL = 16 / sizeof(T), LPB = D / EPL, BPP = 64 * NWS / LPB;
+  constexpr int EPL = 16 / sizeof(T), LPB = D / EPL, BPP = 64 * NW / LPB;
   const int c = threadIdx.x % LPB, G = p.H / p.H_kv;
   double qs[EPL];
 #pragma unroll
@@ -229,26 +268,26 @@ __device__ __forceinline__ const T* means_of(const BlockSelectArgs& p, int64_t o
 // stretch of `per` blocks of it, whose scores go to the workspace.  Bound by the
 // read of the mean keys.
 template <class T, int D, bool SPLIT>
-__global__ __launch_bounds__(64 * NWS) void k_select_row(BlockSelectArgs p, int per) {
+__global__ __launch_bounds__(64 * NWR) void k_select_row(BlockSelectArgs p, int per) {
   extern __shared__ double sc[];
-  __shared__ int sh[3 * NWS];
+  __shared__ PickLds<NWR> sh;
   const int64_t row = blockIdx.x, oi = row / p.H_kv;
   const int g = (int)(row - oi * p.H_kv);
   const RowRange r = row_range(p, oi);
   const int a = max(SPLIT ? (int)blockIdx.y * per : 0, r.f_lo), b = min(SPLIT ? (int)(blockIdx.y + 1) * per : r.nb, r.last0);
   double* out = SPLIT ? p.score + row * p.n_blk : sc;
-  if (r.want > 0 && a < b) score_row<T, D>(p, query_of<T>(p, oi, g, D), means_of<T>(p, oi, g, D), a, b, out);
+  if (r.want > 0 && a < b) score_row<T, D, NWR>(p, query_of<T>(p, oi, g, D), means_of<T>(p, oi, g, D), a, b, out);
   if constexpr (!SPLIT) {
     __syncthreads();
-    pick_row(sc, r, p.top_k, p.idx + row * p.top_k, p.count + row, sh);
+    pick_row<NWR>(sc, r, p.top_k, p.idx + row * p.top_k, p.count + row, sh);
   }
 }
 
 // The lists from scores in the workspace.
-__global__ __launch_bounds__(64 * NWS) void k_select_pick(BlockSelectArgs p) {
-  __shared__ int sh[3 * NWS];
+__global__ __launch_bounds__(64 * NWR) void k_select_pick(BlockSelectArgs p) {
+  __shared__ PickLds<NWR> sh;
   const int64_t row = blockIdx.x;
-  pick_row(p.score + row * p.n_blk, row_range(p, row / p.H_kv), p.top_k, p.idx + row * p.top_k, p.count + row, sh);
+  pick_row<NWR>(p.score + row * p.n_blk, row_range(p, row / p.H_kv), p.top_k, p.idx + row * p.top_k, p.count + row, sh);
 }
 
 __device__ __forceinline__ int pop(bool x) { return (int)__popcll(__ballot(x)); }
@@ -262,13 +301,15 @@ __device__ __forceinline__ u32x2 split_bf16(float a, float b) {   // (hi pair, l
 // turn: the queries, summed over their heads and split into two bf16 terms; the
 // scores [TR][pitch]; fp64 scores of a hard row.
 template <class T, int D>
-__global__ __launch_bounds__(64 * NWS, 2) void k_select_tile(BlockSelectArgs p, int TR, int n_tile, int pitch) {
+__global__ __launch_bounds__(64 * NWS, D <= 128 ? 4 : 2) void k_select_tile(BlockSelectArgs p, int TR, int n_tile, int pitch) {
   constexpr bool BF = sizeof(T) == 2;
   constexpr int NQ = D / 16;
   extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
   __shared__ float qn[32], kn[NWS];
-  __shared__ int sh[3 * NWS], hard[32], n_hard;
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, half = lane >> 5, l31 = lane & 31;
+  __shared__ PickLds<NWS> sh;
+  __shared__ int hard[32], n_hard, seen[32];
+  const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5, l31 = lane & 31;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int64_t og = blockIdx.x / n_tile;
   const int q0 = (int)(blockIdx.x - og * n_tile) * TR, G = p.H / p.H_kv;
   const int64_t o = og / p.H_kv;
@@ -315,7 +356,10 @@ __global__ __launch_bounds__(64 * NWS, 2) void k_select_tile(BlockSelectArgs p, 
   }
   // the most blocks that a row of the tile sees
   int nbm = 0;
-  if (lane < nr) nbm = row_range(p, o * p.n_q + q0 + lane).nb;
+  if (lane < nr) {
+    nbm = row_range(p, o * p.n_q + q0 + lane).nb;
+    if (wave == 0) seen[lane] = nbm;
+  }
 #pragma unroll
   for (int m = 1; m < 64; m <<= 1) nbm = max(nbm, __shfl_xor(nbm, m, 64));
   __syncthreads();
@@ -389,92 +433,94 @@ __global__ __launch_bounds__(64 * NWS, 2) void k_select_tile(BlockSelectArgs p, 
   const uint64_t below = (1ull << lane) - 1;
   for (int r = wave; r < nr; r += NWS) {
     const int64_t oi = o * p.n_q + q0 + r, row = oi * p.H_kv + g;
-    const RowRange rr = row_range(p, oi);
+    const RowRange rr = range_of(p, seen[r]);
     const float* srow = sc + r * pitch;
     int32_t* idx = p.idx + row * p.top_k;
     const float eps2 = keps * (qn[r] + 0x1p-60f) + 0x1p-100f;   // twice the bound
     const int seg = (rr.nb + 63) / 64;
-    auto key_at = [&](int j) -> uint32_t {
+    auto val_at = [&](int j) {   // of the blocks that are to be chosen from
       const int b = 64 * j + lane;
-      return b >= rr.f_lo && b < rr.last0 ? key32(srow[b]) : 0u;
+      return b >= rr.f_lo && b < rr.last0 ? srow[b] : -INFINITY;
     };
-    uint32_t kept[2 * VPL];
+    constexpr int NV = 2 * VPL;
+    float kept[NV];
 #pragma unroll
-    for (int j = 0; j < 2 * VPL; ++j) kept[j] = j < seg ? key_at(j) : 0u;
-    auto reach = [&](uint32_t t) {
-      int n = 0;
+    for (int j = 0; j < NV; ++j) kept[j] = j < seg ? val_at(j) : -INFINITY;
+    auto reach = [&](const float (&t)[3], int (&n)[3]) {
+      n[0] = n[1] = n[2] = 0;
 #pragma unroll
-      for (int j = 0; j < 2 * VPL; ++j)
-        if (j < seg) n += pop(kept[j] >= t);
-      for (int j = 2 * VPL; j < seg; ++j) n += pop(key_at(j) >= t);
-      return n;
+      for (int j = 0; j < NV; ++j)
+        if (j < seg)
+#pragma unroll
+          for (int x = 0; x < 3; ++x) n[x] += pop(kept[j] >= t[x]);
+      for (int j = NV; j < seg; ++j) {
+        const float v = val_at(j);
+#pragma unroll
+        for (int x = 0; x < 3; ++x) n[x] += pop(v >= t[x]);
+      }
     };
-    // scores above w_hi are kept, and `need` of the `cand` ones from w_lo to w_hi
-    uint32_t lo = 1, hi = ~0u;
+    // scores from w_hi on are kept, and `need` of the `cand` ones from w_lo to below it
     bool is_hard = false;
     int cand = 0, need = 0;
-    uint32_t w_lo = 1, w_hi = 0;
+    float w_lo = INFINITY, w_hi = INFINITY;
     if (rr.want > 0) {
       if (!(qn[r] * sqrtf(k2) < 1e38f)) {   // a score may leave the fp32 range, or is no number
         is_hard = true;
       } else {
-        float top = 0.f;
+        // `want` scores reach vlo, fewer reach vhi: quarter until as many as wanted
+        // reach a value or the interval is as short as the error
+        float top = kept[0];
 #pragma unroll
-        for (int j = 0; j < 2 * VPL; ++j) top = fmaxf(top, kept[j] ? __builtin_fabsf(of_key32(kept[j])) : 0.f);
-        for (int j = 2 * VPL; j < seg; ++j) {
-          const uint32_t k = key_at(j);
-          top = fmaxf(top, k ? __builtin_fabsf(of_key32(k)) : 0.f);
-        }
-        top = wave_max(top);
-        float vlo = -1.01f * top, vhi = 1.01f * top;
+        for (int j = 1; j < NV; ++j) top = __builtin_elementwise_maximum(top, kept[j]);
+        for (int j = NV; j < seg; ++j) top = __builtin_elementwise_maximum(top, val_at(j));
+        const float low = wave_min(top);   // 64 scores reach it, if each lane has one
+        float vhi = wave_max(top) + eps2, vlo = rr.want <= 64 && low > -INFINITY ? low : -1.02f * qn[r] * sqrtf(k2) - eps2;
         bool found = false;
-        for (int step = 0; step < 16 && vhi < INFINITY; ++step) {
-          const float v = 0.5f * (vlo + vhi);
-          const uint32_t t = key32(v);
-          if (!(t > lo && t < hi)) break;
-          const int n = reach(t);
-          if (n >= rr.want) {
-            lo = t;
-            vlo = v;
-          } else {
-            hi = t;
-            vhi = v;
-          }
-          if (n == rr.want) {
-            found = true;
-            break;
-          }
-        }
-        while (!found && hi - lo > 1) {
-          const uint32_t t = lo + ((hi - lo) >> 1);
-          const int n = reach(t);
-          if (n >= rr.want) lo = t;
-          else hi = t;
-          found = n == rr.want;
-        }
-        // the want-th score, and the largest below it (or equal to it)
-        uint32_t kth = ~0u, next = 0;
-        for (int j = 0; j < seg; ++j) {
-          const uint32_t k = key_at(j);
-          if (k >= lo) kth = min(kth, k);
-          else next = max(next, k);
-        }
+        float t[3];
+        int n[3];
+        for (int step = 0; step < 64 && vhi - vlo > eps2; ++step) {
+          const float d = 0.25f * (vhi - vlo);
 #pragma unroll
-        for (int m = 1; m < 64; m <<= 1) {
-          kth = min(kth, (uint32_t)__shfl_xor((int)kth, m, 64));
-          next = max(next, (uint32_t)__shfl_xor((int)next, m, 64));
+          for (int x = 0; x < 3; ++x) t[x] = vlo + d * (float)(x + 1);
+          reach(t, n);
+          const int at = (n[0] >= rr.want) + (n[1] >= rr.want) + (n[2] >= rr.want);
+          if (at < 3) vhi = at == 0 ? t[0] : at == 1 ? t[1] : t[2];
+          if (at > 0) {
+            vlo = at == 1 ? t[0] : at == 2 ? t[1] : t[2];
+            found = (at == 1 ? n[0] : at == 2 ? n[1] : n[2]) == rr.want;
+          }
+          if (found) break;
         }
-        const float fk = of_key32(kth);
-        if (!found || (next > 0 && !(fk - of_key32(next) > eps2))) {
-          w_lo = key32(fk - eps2);
-          w_hi = key32(fk + eps2);
-          const int sure = reach(w_hi + 1);
-          cand = reach(w_lo) - sure;
+        if (found) {   // the want-th score and the next
+          float kth = INFINITY, next = -INFINITY;
+#pragma unroll
+          for (int j = 0; j < NV; ++j) {
+            kth = __builtin_elementwise_minimum(kth, kept[j] >= vlo ? kept[j] : INFINITY);
+            next = __builtin_elementwise_maximum(next, kept[j] >= vlo ? -INFINITY : kept[j]);
+          }
+          for (int j = NV; j < seg; ++j) {
+            const float v = val_at(j);
+            kth = fminf(kth, v >= vlo ? v : INFINITY);
+            next = fmaxf(next, v >= vlo ? -INFINITY : v);
+          }
+          kth = wave_min(kth);
+          next = wave_max(next);
+          if (kth - next > eps2) {
+            w_lo = w_hi = kth;   // the scores from kth on are kept
+          } else {
+            vlo = vhi = kth;
+            found = false;
+          }
+        }
+        if (!found) {
+          w_lo = vlo - eps2;
+          w_hi = vhi + eps2;
+          const float t2[3] = {w_lo, __uint_as_float(0x7f800000u), w_hi};
+          reach(t2, n);
+          const int sure = n[2];
+          cand = n[0] - sure;
           need = rr.want - sure;
           is_hard = cand > 64;
-        } else {
-          w_lo = 1;
-          w_hi = kth - 1;   // no block is between
         }
       }
     }
@@ -485,20 +531,23 @@ __global__ __launch_bounds__(64 * NWS, 2) void k_select_tile(BlockSelectArgs p, 
     // fp64 scores of the candidates, the c-th in lane c, and its rank among them
     uint64_t win = 0;   // candidates that are kept, in their order
     if (cand > 0) {
-      double mine = 0.0;
+      constexpr int E = D < 64 ? 1 : D / 64;
+      double qd[E], mine = 0.0;
+#pragma unroll
+      for (int e = 0; e < E; ++e) qd[e] = 0.0;
+      for (int h = 0; h < G; ++h)
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+          if (lane < D) qd[e] += (double)to_f32<T>(gload(qbase + r * p.qs + h * D + lane + 64 * e));
       int c = 0;
       for (int j = 0; j < seg; ++j) {
-        const uint32_t k = key_at(j);
-        uint64_t m = __ballot(k >= w_lo && k <= w_hi);
-        for (; m; m &= m - 1, ++c) {
+        const float v = val_at(j);
+        for (uint64_t m = __ballot(v >= w_lo && v < w_hi); m; m &= m - 1, ++c) {
           const T* kp = km + (int64_t)(64 * j + __builtin_ctzll(m)) * D;
-          const T* qp = qbase + r * p.qs;
           double s = 0.0;
-          for (int d = lane; d < D; d += 64) {
-            double qd = 0.0;
-            for (int h = 0; h < G; ++h) qd += (double)to_f32<T>(qp[h * D + d]);
-            s += qd * (double)to_f32<T>(kp[d]);
-          }
+#pragma unroll
+          for (int e = 0; e < E; ++e)
+            if (lane < D) s += qd[e] * (double)to_f32<T>(gload(kp + lane + 64 * e));
           s = wave_sum64(s);
           if (lane == c) mine = s;
         }
@@ -512,18 +561,23 @@ __global__ __launch_bounds__(64 * NWS, 2) void k_select_tile(BlockSelectArgs p, 
       win = __ballot(lane < cand && rank < need);
     }
     int out = 0, c = 0;
-    for (int j = 0; j < seg; ++j) {
-      const int b = 64 * j + lane;
-      const uint32_t k = rr.want > 0 ? key_at(j) : 0u;
-      const bool in = k >= w_lo && k <= w_hi;
-      const uint64_t im = __ballot(in);
-      const bool keep = (b < rr.nb && (b < rr.f_lo || b >= rr.last0)) || (k > w_hi && k > 0) ||
-                        (in && ((win >> (c + (int)__popcll(im & below))) & 1ull));
-      c += (int)__popcll(im);
-      const uint64_t m = __ballot(keep);
-      if (keep) idx[out + (int)__popcll(m & below)] = b;
+    auto emit = [&](int j, float v) {
+      uint64_t m = __ballot(v >= w_hi) | forced_bits(rr, j);
+      if (cand > 0) {
+        const bool in = v >= w_lo && v < w_hi;
+        const uint64_t im = __ballot(in);
+        if (im) m |= __ballot(in && (win >> (c + (int)__popcll(im & below)) & 1));
+        c += (int)__popcll(im);
+      }
+      if (m == 0) return;
+      const int at = out + (int)__popcll(m & below);
+      if ((m >> lane & 1) && at < p.top_k) idx[at] = 64 * j + lane;
       out += (int)__popcll(m);
-    }
+    };
+#pragma unroll
+    for (int j = 0; j < NV; ++j)
+      if (j < seg) emit(j, kept[j]);
+    for (int j = NV; j < seg; ++j) emit(j, val_at(j));
     for (int t = out + lane; t < p.top_k; t += 64) idx[t] = -1;
     if (lane == 0) p.count[row] = out;
   }
@@ -533,10 +587,10 @@ __global__ __launch_bounds__(64 * NWS, 2) void k_select_tile(BlockSelectArgs p, 
   for (int x = 0; x < n_hard; ++x) {
     const int r = hard[x];
     const int64_t oi = o * p.n_q + q0 + r, row = oi * p.H_kv + g;
-    const RowRange rr = row_range(p, oi);
-    score_row<T, D>(p, qbase + r * p.qs, km, rr.f_lo, rr.last0, sd);
+    const RowRange rr = range_of(p, seen[r]);
+    score_row<T, D, NWS>(p, qbase + r * p.qs, km, rr.f_lo, rr.last0, sd);
     __syncthreads();
-    pick_row(sd, rr, p.top_k, p.idx + row * p.top_k, p.count + row, sh);
+    pick_row<NWS>(sd, rr, p.top_k, p.idx + row * p.top_k, p.count + row, sh);
     __syncthreads();
   }
 }
@@ -549,11 +603,11 @@ hipError_t launch(const BlockSelectArgs& a, const BlockSelectPlan& pl, hipStream
     RS3_LAUNCH(RS3_K_BLOCK_SELECT, st, (k_select_tile<T, D>), dim3((unsigned)n), dim3(64 * NWS), pl.lds, st, a, pl.TR,
                n_tile, pl.pitch);
   } else if (pl.split > 1) {
-    RS3_LAUNCH(RS3_K_BLOCK_SELECT, st, (k_select_row<T, D, true>), dim3((unsigned)a.rows, pl.split), dim3(64 * NWS), 0, st,
+    RS3_LAUNCH(RS3_K_BLOCK_SELECT, st, (k_select_row<T, D, true>), dim3((unsigned)a.rows, pl.split), dim3(64 * NWR), 0, st,
                a, (a.n_blk + pl.split - 1) / pl.split);
-    RS3_LAUNCH(RS3_K_BLOCK_SELECT, st, k_select_pick, dim3((unsigned)a.rows), dim3(64 * NWS), 0, st, a);
+    RS3_LAUNCH(RS3_K_BLOCK_SELECT, st, k_select_pick, dim3((unsigned)a.rows), dim3(64 * NWR), 0, st, a);
   } else {
-    RS3_LAUNCH(RS3_K_BLOCK_SELECT, st, (k_select_row<T, D, false>), dim3((unsigned)a.rows), dim3(64 * NWS), pl.lds, st, a,
+    RS3_LAUNCH(RS3_K_BLOCK_SELECT, st, (k_select_row<T, D, false>), dim3((unsigned)a.rows), dim3(64 * NWR), pl.lds, st, a,
                a.n_blk);
   }
   return hipGetLastError();
