@@ -129,7 +129,7 @@ void select_plan(const rs3_block_shape* s, BlockSelectPlan* a, size_t* ws) {
   a->pitch = (int)((n_blk + 31) / 32 * 32 + 4);
   if (s->n_q >= 8) {
     int TR = 32;
-    while (TR > 4 && (TR * a->pitch * 4 > 81920 - 2048 || TR / 2 >= s->n_q)) TR /= 2;
+    while (TR > 4 && (TR * a->pitch * 4 > 81920 - 6144 || TR / 2 >= s->n_q)) TR /= 2;
     int64_t lds = (int64_t)TR * a->pitch * 4;
     lds = std::max<int64_t>(lds, std::max<int64_t>(n_blk * 8, q_lds));
     if (lds <= SELECT_LDS) {

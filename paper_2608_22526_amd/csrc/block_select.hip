@@ -297,6 +297,49 @@ __device__ __forceinline__ u32x2 split_bf16(float a, float b) {   // (hi pair, l
   return u32x2{hi, pack_bf16x2(a - __uint_as_float(hi << 16), b - __uint_as_float(hi & 0xffff0000u))};
 }
 
+// Quarters (vlo, vhi) until between `want` and `most` of the values reach vlo
+// (true) or the interval is no longer than eps (false).  `want` values reach vlo
+// and fewer reach vhi before and after.  NV values a lane, and more(j) for j from
+// NV below seg.
+template <int NV, class More>
+__device__ __forceinline__ bool narrow(const float (&v)[NV], int seg, More more, int want, int most, float eps, float& vlo,
+                                       float& vhi) {
+  for (int step = 0; step < 64 && vhi - vlo > eps; ++step) {
+    const float d = 0.25f * (vhi - vlo), t0 = vlo + d, t1 = vlo + 2.f * d, t2 = vlo + 3.f * d;
+    int n0 = 0, n1 = 0, n2 = 0;
+#pragma unroll
+    for (int j = 0; j < NV; ++j)
+      if (j < seg) {
+        n0 += pop(v[j] >= t0);
+        n1 += pop(v[j] >= t1);
+        n2 += pop(v[j] >= t2);
+      }
+    for (int j = NV; j < seg; ++j) {
+      const float x = more(j);
+      n0 += pop(x >= t0);
+      n1 += pop(x >= t1);
+      n2 += pop(x >= t2);
+    }
+    int n = most + 1;
+    if (n2 >= want) {
+      vlo = t2;
+      n = n2;
+    } else if (n1 >= want) {
+      vlo = t1;
+      vhi = t2;
+      n = n1;
+    } else if (n0 >= want) {
+      vlo = t0;
+      vhi = t1;
+      n = n0;
+    } else {
+      vhi = t0;
+    }
+    if (n <= most) return true;
+  }
+  return false;
+}
+
 // TR (32, 16, 8 or 4) queries of one (object, key head) per work-group.  LDS, in
 // turn: the queries, summed over their heads and split into two bf16 terms; the
 // scores [TR][pitch]; fp64 scores of a hard row.
@@ -308,6 +351,7 @@ __global__ __launch_bounds__(64 * NWS, D <= 128 ? 4 : 2) void k_select_tile(Bloc
   __shared__ float qn[32], kn[NWS];
   __shared__ PickLds<NWS> sh;
   __shared__ int hard[32], n_hard, seen[32];
+  __shared__ u32x2 few[NWS][64];
   const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5, l31 = lane & 31;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int64_t og = blockIdx.x / n_tile;
@@ -446,18 +490,88 @@ __global__ __launch_bounds__(64 * NWS, D <= 128 ? 4 : 2) void k_select_tile(Bloc
     float kept[NV];
 #pragma unroll
     for (int j = 0; j < NV; ++j) kept[j] = j < seg ? val_at(j) : -INFINITY;
-    auto reach = [&](const float (&t)[3], int (&n)[3]) {
-      n[0] = n[1] = n[2] = 0;
+    // The query in fp64, a stretch of channels per lane, for scores made again.
+    constexpr int E = D < 64 ? 1 : D / 64;
+    double qd[E];
+    auto query64 = [&]() {
+#pragma unroll
+      for (int e = 0; e < E; ++e) qd[e] = 0.0;
+      for (int h = 0; h < G; ++h)
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+          if (lane < D) qd[e] += (double)to_f32<T>(gload(qbase + r * p.qs + h * D + lane + 64 * e));
+    };
+    auto score64 = [&](int b) {
+      const T* kp = km + (int64_t)b * D;
+      double s = 0.0;
+#pragma unroll
+      for (int e = 0; e < E; ++e)
+        if (lane < D) s += qd[e] * (double)to_f32<T>(gload(kp + lane + 64 * e));
+      return wave_sum64(s);
+    };
+    // The scores from t on, one per lane in the order of their blocks; false if
+    // there are more than 64.
+    float x = -INFINITY;
+    int xb = 0;
+    auto compact_row = [&](const float (&v)[NV], int n_seg, auto more, float t) {
+      int n = 0;
+      auto put = [&](int j, float y) {
+        const uint64_t m = __ballot(y >= t);
+        if (m == 0) return;
+        const int at = n + (int)__popcll(m & below);
+        if (y >= t && at < 64) few[wave][at] = u32x2{__float_as_uint(y), (uint32_t)(64 * j + lane)};
+        n += (int)__popcll(m);
+      };
 #pragma unroll
       for (int j = 0; j < NV; ++j)
-        if (j < seg)
-#pragma unroll
-          for (int x = 0; x < 3; ++x) n[x] += pop(kept[j] >= t[x]);
-      for (int j = NV; j < seg; ++j) {
-        const float v = val_at(j);
-#pragma unroll
-        for (int x = 0; x < 3; ++x) n[x] += pop(v >= t[x]);
+        if (j < n_seg) put(j, v[j]);
+      for (int j = NV; j < n_seg; ++j) put(j, more(j));
+      if (n > 64) return false;
+      __builtin_amdgcn_s_waitcnt(0xc07f);   // lgkmcnt(0): written and read by this wave alone
+      __builtin_amdgcn_wave_barrier();
+      const u32x2 y = few[wave][lane];
+      __builtin_amdgcn_wave_barrier();
+      x = lane < n ? __uint_as_float(y[0]) : -INFINITY;
+      xb = (int)y[1];
+      return true;
+    };
+    auto done_row = [&](float vlo, float vhi) {
+      const float one[1] = {x};
+      const bool found = narrow(one, 1, [](int) { return -INFINITY; }, rr.want, rr.want, eps2, vlo, vhi);
+      uint64_t m = __ballot(x >= vlo);
+      bool clear = found;
+      if (found) {
+        const float kth = wave_min(x >= vlo ? x : INFINITY), next = wave_max(x >= vlo ? -INFINITY : x);
+        clear = kth - next > eps2;
+        vlo = vhi = kth;
       }
+      if (!clear) {   // between vlo - eps2 and vhi + eps2 the fp64 scores decide
+        const float w_lo = vlo - eps2, w_hi = vhi + eps2;
+        m = __ballot(x >= w_hi);
+        const uint64_t im = __ballot(x >= w_lo && x < w_hi);
+        const int need = rr.want - (int)__popcll(m);
+        query64();
+        double mine = 0.0;
+        for (uint64_t q = im; q; q &= q - 1) {
+          const int l = __builtin_ctzll(q);
+          const double s = score64(__builtin_amdgcn_readlane(xb, l));
+          if (lane == l) mine = s;
+        }
+        const uint64_t mk = key64(mine);
+        int rank = 0;
+        for (uint64_t q = im; q; q &= q - 1) {
+          const int l = __builtin_ctzll(q);
+          const uint64_t other = (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(mk >> 32), l) << 32 |
+                                 (uint32_t)__builtin_amdgcn_readlane((int)mk, l);
+          rank += other > mk || (other == mk && l < lane);
+        }
+        m |= __ballot((im >> lane & 1) && rank < need);
+      }
+      const int n = rr.f_lo + (int)__popcll(m), at = rr.f_lo + (int)__popcll(m & below);
+      for (int t = lane; t < rr.f_lo; t += 64) idx[t] = t;
+      if ((m >> lane & 1) && at < p.top_k) idx[at] = xb;
+      for (int t = n + lane; t < p.top_k; t += 64) idx[t] = rr.last0 + t - n < rr.nb ? rr.last0 + t - n : -1;
+      if (lane == 0) p.count[row] = n + rr.nb - rr.last0;
     };
     // scores from w_hi on are kept, and `need` of the `cand` ones from w_lo to below it
     bool is_hard = false;
@@ -467,37 +581,29 @@ __global__ __launch_bounds__(64 * NWS, D <= 128 ? 4 : 2) void k_select_tile(Bloc
       if (!(qn[r] * sqrtf(k2) < 1e38f)) {   // a score may leave the fp32 range, or is no number
         is_hard = true;
       } else {
-        // `want` scores reach vlo, fewer reach vhi: quarter until as many as wanted
-        // reach a value or the interval is as short as the error
         float top = kept[0];
 #pragma unroll
-        for (int j = 1; j < NV; ++j) top = __builtin_elementwise_maximum(top, kept[j]);
+        for (int j = 1; j < NV; ++j)
+          if (j < seg) top = __builtin_elementwise_maximum(top, kept[j]);
         for (int j = NV; j < seg; ++j) top = __builtin_elementwise_maximum(top, val_at(j));
         const float low = wave_min(top);   // 64 scores reach it, if each lane has one
         float vhi = wave_max(top) + eps2, vlo = rr.want <= 64 && low > -INFINITY ? low : -1.02f * qn[r] * sqrtf(k2) - eps2;
-        bool found = false;
-        float t[3];
-        int n[3];
-        for (int step = 0; step < 64 && vhi - vlo > eps2; ++step) {
-          const float d = 0.25f * (vhi - vlo);
-#pragma unroll
-          for (int x = 0; x < 3; ++x) t[x] = vlo + d * (float)(x + 1);
-          reach(t, n);
-          const int at = (n[0] >= rr.want) + (n[1] >= rr.want) + (n[2] >= rr.want);
-          if (at < 3) vhi = at == 0 ? t[0] : at == 1 ? t[1] : t[2];
-          if (at > 0) {
-            vlo = at == 1 ? t[0] : at == 2 ? t[1] : t[2];
-            found = (at == 1 ? n[0] : at == 2 ? n[1] : n[2]) == rr.want;
-          }
-          if (found) break;
+        // few are wanted: first a value that at most 48 scores reach, and then on with
+        // those alone, one per lane
+        if (rr.want <= 48 && narrow(kept, seg, val_at, rr.want, 48, eps2, vlo, vhi) &&
+            compact_row(kept, seg, val_at, vlo - eps2)) {
+          done_row(vlo, vhi);
+          continue;
         }
+        bool found = narrow(kept, seg, val_at, rr.want, rr.want, eps2, vlo, vhi);
         if (found) {   // the want-th score and the next
           float kth = INFINITY, next = -INFINITY;
 #pragma unroll
-          for (int j = 0; j < NV; ++j) {
-            kth = __builtin_elementwise_minimum(kth, kept[j] >= vlo ? kept[j] : INFINITY);
-            next = __builtin_elementwise_maximum(next, kept[j] >= vlo ? -INFINITY : kept[j]);
-          }
+          for (int j = 0; j < NV; ++j)
+            if (j < seg) {
+              kth = __builtin_elementwise_minimum(kth, kept[j] >= vlo ? kept[j] : INFINITY);
+              next = __builtin_elementwise_maximum(next, kept[j] >= vlo ? -INFINITY : kept[j]);
+            }
           for (int j = NV; j < seg; ++j) {
             const float v = val_at(j);
             kth = fminf(kth, v >= vlo ? v : INFINITY);
@@ -515,10 +621,19 @@ __global__ __launch_bounds__(64 * NWS, D <= 128 ? 4 : 2) void k_select_tile(Bloc
         if (!found) {
           w_lo = vlo - eps2;
           w_hi = vhi + eps2;
-          const float t2[3] = {w_lo, __uint_as_float(0x7f800000u), w_hi};
-          reach(t2, n);
-          const int sure = n[2];
-          cand = n[0] - sure;
+          int sure = 0, reach = 0;
+#pragma unroll
+          for (int j = 0; j < NV; ++j)
+            if (j < seg) {
+              sure += pop(kept[j] >= w_hi);
+              reach += pop(kept[j] >= w_lo);
+            }
+          for (int j = NV; j < seg; ++j) {
+            const float v = val_at(j);
+            sure += pop(v >= w_hi);
+            reach += pop(v >= w_lo);
+          }
+          cand = reach - sure;
           need = rr.want - sure;
           is_hard = cand > 64;
         }
@@ -531,32 +646,21 @@ __global__ __launch_bounds__(64 * NWS, D <= 128 ? 4 : 2) void k_select_tile(Bloc
     // fp64 scores of the candidates, the c-th in lane c, and its rank among them
     uint64_t win = 0;   // candidates that are kept, in their order
     if (cand > 0) {
-      constexpr int E = D < 64 ? 1 : D / 64;
-      double qd[E], mine = 0.0;
-#pragma unroll
-      for (int e = 0; e < E; ++e) qd[e] = 0.0;
-      for (int h = 0; h < G; ++h)
-#pragma unroll
-        for (int e = 0; e < E; ++e)
-          if (lane < D) qd[e] += (double)to_f32<T>(gload(qbase + r * p.qs + h * D + lane + 64 * e));
+      query64();
+      double mine = 0.0;
       int c = 0;
       for (int j = 0; j < seg; ++j) {
         const float v = val_at(j);
         for (uint64_t m = __ballot(v >= w_lo && v < w_hi); m; m &= m - 1, ++c) {
-          const T* kp = km + (int64_t)(64 * j + __builtin_ctzll(m)) * D;
-          double s = 0.0;
-#pragma unroll
-          for (int e = 0; e < E; ++e)
-            if (lane < D) s += qd[e] * (double)to_f32<T>(gload(kp + lane + 64 * e));
-          s = wave_sum64(s);
+          const double s = score64(64 * j + __builtin_ctzll(m));
           if (lane == c) mine = s;
         }
       }
       const uint64_t mk = key64(mine);
       int rank = 0;
-      for (int x = 0; x < cand; ++x) {
-        const uint64_t other = (uint64_t)__shfl((long long)mk, x, 64);
-        rank += other > mk || (other == mk && x < lane);
+      for (int l = 0; l < cand; ++l) {
+        const uint64_t other = (uint64_t)__shfl((long long)mk, l, 64);
+        rank += other > mk || (other == mk && l < lane);
       }
       win = __ballot(lane < cand && rank < need);
     }
