@@ -48,9 +48,34 @@ __device__ __forceinline__ RowRange row_range(const BlockSelectArgs& p, int64_t 
   return range_of(p, (visible_keys(p.n_vis, oi, p.n_kv) + p.block - 1) / p.block);
 }
 
-__device__ __forceinline__ double wave_sum64(double v) {
-#pragma unroll
-  for (int m = 1; m < 64; m <<= 1) v += __shfl_xor(v, m, 64);
+// Sum over groups of N lanes (a power of two from 4 on), the same bits in every
+// lane: the exchanges of wave_sum on both halves of the values.
+template <int CTRL>
+__device__ __forceinline__ double dppd(double v) {
+  const uint64_t u = (uint64_t)__double_as_longlong(v);
+  const uint32_t lo = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)u, CTRL, 0xF, 0xF, false);
+  const uint32_t hi = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)(u >> 32), CTRL, 0xF, 0xF, false);
+  return __longlong_as_double((long long)((uint64_t)hi << 32 | lo));
+}
+template <int N>
+__device__ __forceinline__ double group_sum64(double v) {
+  v += dppd<0xB1>(v);
+  v += dppd<0x4E>(v);
+  if constexpr (N >= 8) v += dppd<0x141>(v);
+  if constexpr (N >= 16) v += dppd<0x140>(v);
+  auto both = [](uint32_t lo, uint32_t hi) { return __longlong_as_double((long long)((uint64_t)hi << 32 | lo)); };
+  if constexpr (N >= 32) {
+    const uint64_t u = (uint64_t)__double_as_longlong(v);
+    const auto a = __builtin_amdgcn_permlane16_swap((uint32_t)u, (uint32_t)u, false, false);
+    const auto b = __builtin_amdgcn_permlane16_swap((uint32_t)(u >> 32), (uint32_t)(u >> 32), false, false);
+    v = both(a[0], b[0]) + both(a[1], b[1]);
+  }
+  if constexpr (N >= 64) {
+    const uint64_t u = (uint64_t)__double_as_longlong(v);
+    const auto a = __builtin_amdgcn_permlane32_swap((uint32_t)u, (uint32_t)u, false, false);
+    const auto b = __builtin_amdgcn_permlane32_swap((uint32_t)(u >> 32), (uint32_t)(u >> 32), false, false);
+    v = both(a[0], b[0]) + both(a[1], b[1]);
+  }
   return v;
 }
 
@@ -68,18 +93,25 @@ __device__ __forceinline__ uint64_t forced_bits(const RowRange& r, int j) {
   return range_bits(j, 0, r.f_lo) | range_bits(j, r.last0, r.nb);
 }
 
-// LDS of pick_row: three counters in turn, and a word or two per wave.
+// LDS of pick_row: three counters in turn, a word or two per wave, and the
+// counts of BINS intervals and the few scores of the short way.
+constexpr int BINS = 256;
 template <int NW>
 struct PickLds {
   unsigned long long n[3];
   float f[2 * NW];
+  uint32_t bin[BINS];
+  uint64_t key[64];
+  int block[64];
 };
 
 // The list of one row from its fp64 scores, by a work-group of NW waves: the
 // largest key that `want` scores reach, by quartering (first of the values, which
 // needs few steps for ordinary scores, then of the keys, which always ends),
 // then the blocks above it and the lowest of those at it.  A wave owns a stretch
-// of blocks.
+// of blocks.  The short way, for finite scores of which a few are wanted: they
+// are counted in BINS intervals from the largest down, and if at most 64 lie in
+// the interval of the want-th and above, one wave ranks those.
 template <int NW>
 __device__ void pick_row(const double* sc, const RowRange& r, int top_k, int32_t* idx, int32_t* count, PickLds<NW>& sh) {
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -95,6 +127,7 @@ __device__ void pick_row(const double* sc, const RowRange& r, int top_k, int32_t
   // scores at or above t[0..2], over the work-group: 21 bits of a counter each
   int slot = 0;
   if (tid < 3) sh.n[tid] = 0;
+  for (int x = tid; x < BINS; x += 64 * NW) sh.bin[x] = 0;
   auto reach = [&](const uint64_t (&t)[3], int (&n)[3]) {
     n[0] = n[1] = n[2] = 0;
 #pragma unroll
@@ -136,6 +169,88 @@ __device__ void pick_row(const double* sc, const RowRange& r, int top_k, int32_t
     __syncthreads();
     top = wave_max(sh.f[lane % NW]);
     low = wave_min(sh.f[NW + lane % NW]);
+    if (seg <= VPL && r.want <= 48 && top > low && top - low < INFINITY) {
+      const float scale = (float)(BINS - 1) / (top - low);
+      // interval of a score, 0 the highest; the scores below `low` (or no numbers) count as the last
+      auto bin_of = [&](uint64_t k) {
+        const float y = (top - (float)of_key64(k)) * scale;
+        return y < (float)(BINS - 1) ? (int)fmaxf(y, 0.f) : BINS - 1;
+      };
+#pragma unroll
+      for (int j = 0; j < VPL; ++j)
+        if (j < seg && kept[j]) atomicAdd(&sh.bin[bin_of(kept[j])], 1u);
+      __syncthreads();
+      // every wave: the first interval that, with those before it, holds `want`
+      uint32_t c[BINS / 64], mine = 0;
+#pragma unroll
+      for (int x = 0; x < BINS / 64; ++x) mine += c[x] = sh.bin[lane * (BINS / 64) + x];
+      uint32_t incl = mine;
+#pragma unroll
+      for (int d = 1; d < 64; d <<= 1) {
+        const uint32_t up = __shfl_up(incl, d, 64);
+        if (lane >= d) incl += up;
+      }
+      const uint64_t enough = __ballot((int)incl >= r.want);
+      int last = BINS, n_few = 0;
+      if (enough) {
+        const int l = __builtin_ctzll(enough);
+        uint32_t sum = incl - mine;
+        int at = BINS;
+        uint32_t total = 0;
+#pragma unroll
+        for (int x = BINS / 64 - 1; x >= 0; --x) {
+          uint32_t upto = sum;
+#pragma unroll
+          for (int y = 0; y <= x; ++y) upto += c[y];
+          if ((int)upto >= r.want) {
+            at = lane * (BINS / 64) + x;
+            total = upto;
+          }
+        }
+        last = __builtin_amdgcn_readlane(at, l);
+        n_few = __builtin_amdgcn_readlane((int)total, l);
+      }
+      if (last < BINS - 1 && n_few <= 64) {
+        // those scores in the order of their blocks
+        int n = 0;
+#pragma unroll
+        for (int j = 0; j < VPL; ++j)
+          if (j < seg) n += (int)__popcll(__ballot(kept[j] && bin_of(kept[j]) <= last));
+        if (lane == 0) sh.f[wave] = (float)n;
+        __syncthreads();
+        int at = (int)wave_sum(lane < wave ? sh.f[lane % NW] : 0.f);
+#pragma unroll
+        for (int j = 0; j < VPL; ++j)
+          if (j < seg) {
+            const bool in = kept[j] && bin_of(kept[j]) <= last;
+            const uint64_t m = __ballot(in);
+            const int to = at + (int)__popcll(m & below);
+            if (in && to < 64) {
+              sh.key[to] = kept[j];
+              sh.block[to] = 64 * (j0 + j) + lane;
+            }
+            at += (int)__popcll(m);
+          }
+        __syncthreads();
+        if (wave == 0) {
+          const uint64_t k = lane < n_few ? sh.key[lane] : 0ull;
+          const int b = sh.block[lane];
+          int rank = 0;
+          for (int x = 0; x < n_few; ++x) {
+            const uint64_t other = sh.key[x];
+            rank += other > k || (other == k && x < lane);
+          }
+          const uint64_t m = __ballot(lane < n_few && rank < r.want);
+          const int to = r.f_lo + (int)__popcll(m & below), free_end = r.f_lo + r.want;
+          for (int t = lane; t < r.f_lo; t += 64) idx[t] = t;
+          if ((m >> lane & 1) && to < top_k) idx[to] = b;
+          for (int t = free_end + lane; t < top_k; t += 64)
+            idx[t] = r.last0 + t - free_end < r.nb ? r.last0 + t - free_end : -1;
+          if (lane == 0) *count = min(top_k, r.nb);
+        }
+        return;
+      }
+    }
     const double room = 1e-3 * ((double)top - low) + 1e-6 * fabs(top);
     double vlo = low - room, vhi = top + room;
     bool found = false;
@@ -236,8 +351,7 @@ __device__ void score_row(const BlockSelectArgs& p, const T* q, const T* km, int
       double s = 0.0;
 #pragma unroll
       for (int e = 0; e < EPL; ++e) s += qs[e] * (double)chunk_val<T>(v[u], e);
-#pragma unroll
-      for (int m = 1; m < LPB; m <<= 1) s += __shfl_xor(s, m, 64);
+      s = group_sum64<LPB>(s);
       if (__any(!(fabs(s) < INFINITY))) {
         double t = 0.0;
         for (int h = 0; h < G; ++h) {
@@ -245,8 +359,7 @@ __device__ void score_row(const BlockSelectArgs& p, const T* q, const T* km, int
 #pragma unroll
           for (int e = 0; e < EPL; ++e) t += (double)chunk_val<T>(w, e) * (double)chunk_val<T>(v[u], e);
         }
-#pragma unroll
-        for (int m = 1; m < LPB; m <<= 1) t += __shfl_xor(t, m, 64);
+        t = group_sum64<LPB>(t);
         s = fabs(s) < INFINITY ? s : t;
       }
       if (c == 0 && b0 + u * BPP < b) sc[b0 + u * BPP] = s;
@@ -507,7 +620,7 @@ __global__ __launch_bounds__(64 * NWS, D <= 128 ? 4 : 2) void k_select_tile(Bloc
 #pragma unroll
       for (int e = 0; e < E; ++e)
         if (lane < D) s += qd[e] * (double)to_f32<T>(gload(kp + lane + 64 * e));
-      return wave_sum64(s);
+      return group_sum64<64>(s);
     };
     // The scores from t on, one per lane in the order of their blocks; false if
     // there are more than 64.
