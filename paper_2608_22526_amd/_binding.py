@@ -422,14 +422,25 @@ def _check_rows(name: str, t, last: int, dtype, device):
                          % (name, room, t.dtype, t.device, last, dtype, device))
 
 
-def _torch_dtype(dt: int):
+def _call():
+    """The current device and its current stream's handle."""
     import torch
-    return torch.bfloat16 if dt == RS3_BF16 else torch.float32
+    C = torch._C
+    dev = C._cuda_getDevice()
+    return torch, dev, C._cuda_getCurrentRawStream(dev)
 
 
-def _call_device():
-    import torch
-    return torch.device("cuda", torch.cuda.current_device())
+def _tensor(torch, name: str, t, numel: int, dtype, dev: int):
+    if t.numel() >= numel and t.dtype is dtype and t.get_device() == dev and t.is_contiguous():
+        return t.data_ptr()
+    _check_tensor(name, t, numel, dtype, torch.device("cuda", dev))
+    return t.data_ptr()
+
+
+def _rows(torch, name: str, t, last: int, dtype, dev: int):
+    if not (t.numel() >= last and t.dtype is dtype and t.get_device() == dev and t.is_contiguous()):
+        _check_rows(name, t, last, dtype, torch.device("cuda", dev))
+    return t.data_ptr()
 
 
 def qk_norm_rope(n: int, Q, H: int, K, H_kv: int, d_h: int, dtype: int, Qo, Ko, gain_q=None, gain_k=None,
@@ -438,26 +449,34 @@ def qk_norm_rope(n: int, Q, H: int, K, H_kv: int, d_h: int, dtype: int, Qo, Ko, 
                  ko_stride: Optional[int] = None, stream=None):
     """RMS norm of each head of Q [n][H][d_h] and K [n][H_kv][d_h] (None with
     0 heads) and the rotation of its first d_rot channels by table[pos]."""
-    import torch
-    dev, dt, f32 = _call_device(), _torch_dtype(dtype), torch.float32
-    qs, ks = H * d_h if q_stride is None else q_stride, H_kv * d_h if k_stride is None else k_stride
-    qos, kos = H * d_h if qo_stride is None else qo_stride, H_kv * d_h if ko_stride is None else ko_stride
-    if n > 0:
-        for name, t, stride, heads in (("Q", Q, qs, H), ("Qo", Qo, qos, H), ("K", K, ks, H_kv), ("Ko", Ko, kos, H_kv)):
-            if t is not None and heads > 0:
-                _check_rows(name, t, (n - 1) * stride + heads * d_h, dt, dev)
-    for name, t in (("gain_q", gain_q), ("gain_k", gain_k)):
-        if t is not None:
-            _check_tensor(name, t, d_h, f32, dev)
+    torch, dev, st = _call()
+    dt, f32 = torch.bfloat16 if dtype == RS3_BF16 else torch.float32, torch.float32
+    wq, wk = H * d_h, H_kv * d_h
+    qs, ks = wq if q_stride is None else q_stride, wk if k_stride is None else k_stride
+    qos, kos = wq if qo_stride is None else qo_stride, wk if ko_stride is None else ko_stride
+    q = k = qo = ko = gq = gk = tab = ps = None
     n_pos = 0
+    if n > 0 and wq > 0:
+        if Q is not None:
+            q = _rows(torch, "Q", Q, (n - 1) * qs + wq, dt, dev)
+        if Qo is not None:
+            qo = _rows(torch, "Qo", Qo, (n - 1) * qos + wq, dt, dev)
+    if n > 0 and wk > 0:
+        if K is not None:
+            k = _rows(torch, "K", K, (n - 1) * ks + wk, dt, dev)
+        if Ko is not None:
+            ko = _rows(torch, "Ko", Ko, (n - 1) * kos + wk, dt, dev)
+    if gain_q is not None:
+        gq = _tensor(torch, "gain_q", gain_q, d_h, f32, dev)
+    if gain_k is not None:
+        gk = _tensor(torch, "gain_k", gain_k, d_h, f32, dev)
     if table is not None:
         n_pos = table.shape[0]
-        _check_tensor("table", table, n_pos * d_rot, f32, dev)
+        tab = _tensor(torch, "table", table, n_pos * d_rot, f32, dev)
     if pos is not None:
-        _check_tensor("pos", pos, n, torch.int32, dev)
-    _check(lib().rs3_qk_norm_rope(n, _ptr(Q), qs, H, _ptr(K), ks, H_kv, d_h, dtype, _ptr(gain_q), _ptr(gain_k), eps,
-                                  _ptr(table), n_pos, d_rot, pairing, _ptr(pos), _ptr(Qo), qos, _ptr(Ko), kos,
-                                  _stream(stream)), "rs3_qk_norm_rope")
+        ps = _tensor(torch, "pos", pos, n, torch.int32, dev)
+    _check(lib().rs3_qk_norm_rope(n, q, qs, H, k, ks, H_kv, d_h, dtype, gq, gk, eps, tab, n_pos, d_rot, pairing, ps,
+                                  qo, qos, ko, kos, st if stream is None else stream), "rs3_qk_norm_rope")
 
 
 def block_shape(dtype: int, n_obj: int, n_q: int, n_kv: int, H: int, H_kv: int, d_h: int, block: int, top_k: int,
@@ -474,27 +493,29 @@ def block_shape(dtype: int, n_obj: int, n_q: int, n_kv: int, H: int, H_kv: int, 
     return s
 
 
-def _block_rows(s: BlockShape, name: str, t, x: str, rows: int, heads: int, dev):
-    if rows > 0 and s.n_obj > 0:
-        _check_rows(name, t, (s.n_obj - 1) * getattr(s, x + "_obj_stride") + (rows - 1) * getattr(s, x + "_stride") +
-                    heads * s.d_h, _torch_dtype(s.dt), dev)
+def _span(n_obj: int, obj: int, rows: int, row: int, width: int) -> int:
+    """Elements from the first to the last of strided rows."""
+    return (n_obj - 1) * obj + (rows - 1) * row + width if rows > 0 and n_obj > 0 else 0
 
 
-def _block_means_numel(s: BlockShape) -> int:
-    return s.n_obj * s.H_kv * ((s.n_kv + s.block - 1) // s.block if s.block > 0 else 0) * s.d_h
+def _means(torch, s: BlockShape, Kmean, dt, dev: int):
+    n_blk = (s.n_kv + s.block - 1) // s.block if s.block > 0 else 0
+    return _tensor(torch, "Kmean", Kmean, s.n_obj * s.H_kv * n_blk * s.d_h, dt, dev)
+
+
+def _shape_dtype(torch, s: BlockShape):
+    return torch.bfloat16 if s.dt == RS3_BF16 else torch.float32
 
 
 def block_means(shape: BlockShape, K, Kmean, kv_len=None, n_new: int = 0, stream=None):
     """Kmean [n_obj][H_kv][n_blk][d_h]: the mean key of every block of K, or
     (n_new > 0) of the blocks that hold each object's last n_new keys."""
-    import torch
-    dev = _call_device()
-    _block_rows(shape, "K", K, "k", shape.n_kv, shape.H_kv, dev)
-    _check_tensor("Kmean", Kmean, _block_means_numel(shape), _torch_dtype(shape.dt), dev)
-    if kv_len is not None:
-        _check_tensor("kv_len", kv_len, shape.n_obj, torch.int32, dev)
-    _check(lib().rs3_block_means(ctypes.byref(shape), _ptr(K), _ptr(kv_len), n_new, _ptr(Kmean), _stream(stream)),
-           "rs3_block_means")
+    torch, dev, st = _call()
+    s, dt = shape, _shape_dtype(torch, shape)
+    k = _rows(torch, "K", K, _span(s.n_obj, s.k_obj_stride, s.n_kv, s.k_stride, s.H_kv * s.d_h), dt, dev)
+    m = _means(torch, s, Kmean, dt, dev)
+    n = None if kv_len is None else _tensor(torch, "kv_len", kv_len, s.n_obj, torch.int32, dev)
+    _check(lib().rs3_block_means(s, k, n, n_new, m, st if stream is None else stream), "rs3_block_means")
 
 
 def block_select_workspace_size(shape: BlockShape) -> int:
@@ -504,33 +525,31 @@ def block_select_workspace_size(shape: BlockShape) -> int:
     return out.value
 
 
-def _check_lists(shape: BlockShape, idx, count, n_vis, dev):
-    import torch
-    rows = shape.n_obj * shape.n_q
-    _check_tensor("idx", idx, rows * shape.H_kv * shape.top_k, torch.int32, dev)
-    _check_tensor("count", count, rows * shape.H_kv, torch.int32, dev)
-    if n_vis is not None:
-        _check_tensor("n_vis", n_vis, rows, torch.int32, dev)
+def _lists(torch, s: BlockShape, idx, count, n_vis, dev: int):
+    rows, i32 = s.n_obj * s.n_q, torch.int32
+    lists = rows * s.H_kv
+    return (_tensor(torch, "idx", idx, lists * s.top_k, i32, dev), _tensor(torch, "count", count, lists, i32, dev),
+            None if n_vis is None else _tensor(torch, "n_vis", n_vis, rows, i32, dev))
 
 
-def _workspace(ws, dev):
+def _workspace(ws, dev: int):
     if ws is None:
         return None, 0
-    if ws.device != dev or not ws.is_contiguous():
-        raise ValueError("ws: on %s, need contiguous memory on %s" % (ws.device, dev))
+    if ws.get_device() != dev or not ws.is_contiguous():
+        raise ValueError("ws: on %s, need contiguous memory on cuda:%d" % (ws.device, dev))
     return ws.data_ptr(), ws.numel() * ws.element_size()
 
 
 def block_select(shape: BlockShape, Q, Kmean, idx, count, n_vis=None, ws=None, stream=None):
     """Each query's blocks by the scores of their mean keys: idx int32
     [n_obj][n_q][H_kv][top_k] ascending (-1 past the count), count int32."""
-    dev = _call_device()
-    _block_rows(shape, "Q", Q, "q", shape.n_q, shape.H, dev)
-    _check_tensor("Kmean", Kmean, _block_means_numel(shape), _torch_dtype(shape.dt), dev)
-    _check_lists(shape, idx, count, n_vis, dev)
+    torch, dev, st = _call()
+    s, dt = shape, _shape_dtype(torch, shape)
+    q = _rows(torch, "Q", Q, _span(s.n_obj, s.q_obj_stride, s.n_q, s.q_stride, s.H * s.d_h), dt, dev)
+    m = _means(torch, s, Kmean, dt, dev)
+    i, c, v = _lists(torch, s, idx, count, n_vis, dev)
     p, nbytes = _workspace(ws, dev)
-    _check(lib().rs3_block_select(ctypes.byref(shape), _ptr(Q), _ptr(Kmean), _ptr(n_vis), _ptr(idx), _ptr(count), p,
-                                  nbytes, _stream(stream)), "rs3_block_select")
+    _check(lib().rs3_block_select(s, q, m, v, i, c, p, nbytes, st if stream is None else stream), "rs3_block_select")
 
 
 def block_attend_workspace_size(shape: BlockShape) -> int:
@@ -542,15 +561,17 @@ def block_attend_workspace_size(shape: BlockShape) -> int:
 
 def block_attend(shape: BlockShape, Q, K, V, idx, count, O, n_vis=None, ws=None, stream=None):
     """Softmax attention of every query over the keys of its listed blocks."""
-    dev = _call_device()
-    _block_rows(shape, "Q", Q, "q", shape.n_q, shape.H, dev)
-    _block_rows(shape, "K", K, "k", shape.n_kv, shape.H_kv, dev)
-    _block_rows(shape, "V", V, "v", shape.n_kv, shape.H_kv, dev)
-    _block_rows(shape, "O", O, "o", shape.n_q, shape.H, dev)
-    _check_lists(shape, idx, count, n_vis, dev)
+    torch, dev, st = _call()
+    s, dt = shape, _shape_dtype(torch, shape)
+    n_obj, n_q, n_kv, wq, wk = s.n_obj, s.n_q, s.n_kv, s.H * s.d_h, s.H_kv * s.d_h
+    q = _rows(torch, "Q", Q, _span(n_obj, s.q_obj_stride, n_q, s.q_stride, wq), dt, dev)
+    k = _rows(torch, "K", K, _span(n_obj, s.k_obj_stride, n_kv, s.k_stride, wk), dt, dev)
+    v = _rows(torch, "V", V, _span(n_obj, s.v_obj_stride, n_kv, s.v_stride, wk), dt, dev)
+    o = _rows(torch, "O", O, _span(n_obj, s.o_obj_stride, n_q, s.o_stride, wq), dt, dev)
+    i, c, vis = _lists(torch, s, idx, count, n_vis, dev)
     p, nbytes = _workspace(ws, dev)
-    _check(lib().rs3_block_attend(ctypes.byref(shape), _ptr(Q), _ptr(K), _ptr(V), _ptr(idx), _ptr(count), _ptr(n_vis),
-                                  _ptr(O), p, nbytes, _stream(stream)), "rs3_block_attend")
+    _check(lib().rs3_block_attend(s, q, k, v, i, c, vis, o, p, nbytes, st if stream is None else stream),
+           "rs3_block_attend")
 
 
 class Stack:

@@ -11,7 +11,7 @@ struct QkNormArgs {
   void* Y[2];
   int64_t xs[2], ys[2];  // elements between rows
   const float* gain[2];  // [d_h] or null
-  int heads[2];
+  int heads[2], chunks[2];   // chunks: of heads that a group of lanes takes together
   int n, d_h, d_rot, halves, n_pos;
   float eps, inv_d;
   const float* table;    // [n_pos][d_rot/2][2] or null
