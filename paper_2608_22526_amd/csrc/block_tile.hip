@@ -18,6 +18,8 @@ namespace rs3 {
 typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
 
 
+constexpr int XCD_RUN = 8;
+
 // The blocks' counters to 0 (a kernel, which a graph can hold).
 __global__ __launch_bounds__(256) void k_block_zero(uint32_t* total, int64_t n) {
   const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
@@ -34,24 +36,39 @@ __global__ __launch_bounds__(512) void k_block_count(BlockAttendArgs p, BlockTil
   const int items = max(min(w.run, min((ch + 1) * w.chunk, p.n_q) - q0), 0) * p.top_k;
   for (int b = tid; b < p.n_blk; b += 512) sc[b] = 0;
   __syncthreads();
-  for (int e = tid; e < items; e += 512) {
-    const int iq = e / p.top_k, t = e - iq * p.top_k;
-    const int64_t oi = (int64_t)o * p.n_q + q0 + iq, row = oi * p.H_kv + hk;
-    const int32_t* list = p.idx + row * p.top_k;
-    const int b = gload(list + t), prev = gload(list + max(t - 1, 0)), cnt = min(gload(p.count + row), p.top_k);
-    const bool ok = t < cnt && b >= 0 && b < p.n_blk && (t == 0 || b > prev) &&
-                    (int64_t)b * p.block < visible_keys(p.n_vis, oi, p.n_kv);
-    uint32_t at = ~0u;
-    if (ok) {
-      at = atomicAdd(&sc[b], 1u) * BLOCK_TILE_MAX + (uint32_t)b;
-    } else {
-      float* ml = part.ML + (row * p.top_k + t) * p.G * 2;
-      for (int g = 0; g < p.G; ++g) {
-        ml[2 * g] = -INFINITY;
-        ml[2 * g + 1] = 0.f;
-      }
+  constexpr int U = 4;   // entries of a thread in flight
+  for (int e0 = tid; e0 < items; e0 += U * 512) {
+    int b[U], prev[U], cnt[U], vis[U], t[U];
+    int64_t row[U];
+#pragma unroll
+    for (int k = 0; k < U; ++k) {
+      const int e = min(e0 + 512 * k, items - 1), iq = e / p.top_k;
+      const int64_t oi = (int64_t)o * p.n_q + q0 + iq;
+      t[k] = e - iq * p.top_k;
+      row[k] = oi * p.H_kv + hk;
+      const int32_t* list = p.idx + row[k] * p.top_k;
+      b[k] = gload(list + t[k]);
+      prev[k] = gload(list + max(t[k] - 1, 0));
+      cnt[k] = gload(p.count + row[k]);
+      vis[k] = visible_keys(p.n_vis, oi, p.n_kv);
     }
-    w.ord[((int64_t)grp * p.n_q + q0) * p.top_k + e] = at;
+#pragma unroll
+    for (int k = 0; k < U; ++k) {
+      if (e0 + 512 * k >= items) break;
+      const bool ok = t[k] < min(cnt[k], p.top_k) && b[k] >= 0 && b[k] < p.n_blk && (t[k] == 0 || b[k] > prev[k]) &&
+                      (int64_t)b[k] * p.block < vis[k];
+      uint32_t at = ~0u;
+      if (ok) {
+        at = atomicAdd(&sc[b[k]], 1u) * BLOCK_TILE_MAX + (uint32_t)b[k];
+      } else {
+        float* ml = part.ML + (row[k] * p.top_k + t[k]) * p.G * 2;
+        for (int g = 0; g < p.G; ++g) {
+          ml[2 * g] = -INFINITY;
+          ml[2 * g + 1] = 0.f;
+        }
+      }
+      w.ord[((int64_t)grp * p.n_q + q0) * p.top_k + e0 + 512 * k] = at;
+    }
   }
   __syncthreads();
   // the run's place among the chunk's: in the order in which the runs come by,
@@ -228,8 +245,7 @@ struct TileLayout {
 // NW waves of 32 rows; NT 32-key tiles per stage; ONE: the block is one stage.
 // Logits transposed, S^T = K Q^T, so that the weights feed O^T += V^T P^T from
 // their registers (in bf16 the value operand comes from the rows of V by
-// transposed LDS reads); a row of the partial is one lane pair.  Consecutive
-// tiles of a group go to one XCD.
+// transposed LDS reads); a row of the partial is one lane pair.
 template <class T, int D, int NT, int NW, bool ONE>
 __global__ __launch_bounds__(64 * NW, D * sizeof(T) <= 256 ? (D * sizeof(T) <= 128 || ONE ? 4 : 3) : 1) void k_block_tile(
     BlockAttendArgs p, BlockTileArgs w, BlockPartArgs part) {
@@ -237,8 +253,10 @@ __global__ __launch_bounds__(64 * NW, D * sizeof(T) <= 256 ? (D * sizeof(T) <= 1
   constexpr bool BF = sizeof(T) == 2;
   constexpr int CPR = L::CPR, NDT = D / 32, NQ = BF ? D / 16 : D / 8, TH = 64 * NW;
   extern __shared__ __attribute__((aligned(1024))) uint8_t lds[];
-  const int64_t n_item = (int64_t)w.groups * w.tcap, per = (n_item + 7) / 8;
-  const int64_t it = (blockIdx.x & 7) * per + (blockIdx.x >> 3);
+  // XCD_RUN consecutive tiles, mostly of one block, go to one XCD and its L2
+  const int64_t n_item = (int64_t)w.groups * w.tcap;
+  const int turn = blockIdx.x >> 3;
+  const int64_t it = ((int64_t)(turn / XCD_RUN) * 8 + (blockIdx.x & 7)) * XCD_RUN + turn % XCD_RUN;
   if (it >= n_item) return;
   const int grp = (int)(it / w.tcap);
   const int64_t tile = (int64_t)w.ch * n_item + it;
@@ -497,7 +515,7 @@ __global__ __launch_bounds__(64 * NW, D * sizeof(T) <= 256 ? (D * sizeof(T) <= 1
 template <class T, int D, int NT, bool ONE>
 hipError_t launch_stages(const BlockAttendArgs& a, const BlockTileArgs& t, const BlockPartArgs& w, hipStream_t st) {
   constexpr int NW = BLOCK_TILE_WAVES;
-  const int64_t per = ((int64_t)t.groups * t.tcap + 7) / 8;
+  const int64_t per = ((int64_t)t.groups * t.tcap + 8 * XCD_RUN - 1) / (8 * XCD_RUN) * XCD_RUN;
   RS3_LAUNCH(RS3_K_BLOCK_ATTEND, st, (k_block_tile<T, D, NT, NW, ONE>), dim3((unsigned)(8 * per)), dim3(64 * NW),
              (TileLayout<T, D, NT, NW>::BYTES), st, a, t, w);
   return hipGetLastError();
