@@ -75,7 +75,22 @@ void attend_plan(const rs3_block_shape* s, AttendPlan* a) {
     return at;
   };
   const size_t per_q = (size_t)s->n_obj * s->H * s->top_k * s->d_h * elem(s->dt);   // partial rows of one query
-  a->tile = s->n_q >= 64 && n_blk <= BLOCK_TILE_MAX && n_blk > 0 && per_q <= (16u << 20) && G <= 32 * BLOCK_TILE_WAVES;
+  // What the row form reads: the keys and values of each row's blocks, and as much
+  // time as 128 KiB more for the row itself. The tile form reads each once, but has
+  // five launches and the partial rows. Against 320 MiB and twice the cache (row and
+  // tile form in us, 64-key blocks, bf16):
+  //   1 x n_q, 32/8 heads of 128, 16 of 256 blocks: n_q 32 16/31, 64 28/33, 128 52/37, 256 99/43
+  //   8 x n_q, the same of 128 blocks: n_q 8 34/49, 16 53/61, 32 95/74, 64 182/87
+  //   1 x n_q, 8/2 heads, 16 of 4096 blocks: n_q 256 42/62, 512 77/75, 1024 145/86
+  //   64 x n_q, 8/8 heads of 128, all 4 blocks: n_q 8 86/31, 64 622/44
+  //   1 x n_q, 8/8 heads of 64, fp32, 16 of 128 blocks of 32: n_q 32 12/24, 64 22/25, 128 41/27
+  const int64_t rows = (int64_t)s->n_obj * s->n_q * s->H_kv * ((G + 15) / 16);
+  const int64_t key_bytes = (int64_t)2 * s->d_h * elem(s->dt);
+  const int64_t keys = std::min<int64_t>((int64_t)s->top_k * s->block, s->n_kv);
+  const double row_reads = (double)rows * (keys * key_bytes + (128 << 10));
+  const double tile_reads = (320 << 20) + 2.0 * s->n_obj * s->H_kv * s->n_kv * key_bytes;
+  a->tile = s->n_q >= 8 && row_reads > tile_reads && n_blk <= BLOCK_TILE_MAX && n_blk > 0 && per_q <= (16u << 20) &&
+            G <= 32 * BLOCK_TILE_WAVES;
   if (a->tile) {
     const int64_t most_q = std::min<int64_t>(1 << 20, std::max<int64_t>(64, (int64_t)(PART_BYTES / per_q)));
     a->chunks = (int)((s->n_q + most_q - 1) / most_q);
@@ -96,7 +111,6 @@ void attend_plan(const rs3_block_shape* s, AttendPlan* a) {
     a->ml = take((size_t)s->n_q * s->top_k * s->H * s->n_obj * 8);
   } else {
     // a work-group per CU, each with a few pieces of 32 keys per wave
-    const int64_t rows = (int64_t)s->n_obj * s->n_q * s->H_kv * ((G + 15) / 16);
     int64_t S = rows > 0 ? 256 / rows : 1;
     const int64_t most = (int64_t)s->top_k * s->block / 32 / 8;
     S = S < most ? S : most;
@@ -123,13 +137,19 @@ void select_plan(const rs3_block_shape* s, BlockSelectPlan* a, size_t* ws) {
   *ws = 0;
   const int64_t n_blk = n_blocks(s), rows = (int64_t)s->n_obj * s->n_q * s->H_kv;
   a->split = 1;
-  // Several queries: the largest tile whose scores leave room for two work-groups
-  // per CU, at least four queries.
+  // Several queries (us, row form and tile form at 16 of 256 blocks, 8 key heads of
+  // 128: 256 rows 10.4/10.7, 512 19/11, 1024 36/11, 4096 131/15). The row form has a
+  // work-group per row, so up to one per CU it is no slower, and at many blocks faster
+  // (256 rows of 4096 blocks 49/94). The tile: the largest whose scores leave room for
+  // two work-groups per CU, smaller while that gives fewer work-groups than CUs (64
+  // queries: tiles of 32 19.5, of 4 10.8), at least four queries.
   const int q_lds = 2 * 32 * s->d_h * 2;   // the queries' two terms
   a->pitch = (int)((n_blk + 31) / 32 * 32 + 4);
-  if (s->n_q >= 8) {
+  if (s->n_q >= 4 && (rows > 256 || (s->n_q >= 8 && n_blk <= 256))) {
     int TR = 32;
-    while (TR > 4 && (TR * a->pitch * 4 > 81920 - 6144 || TR / 2 >= s->n_q)) TR /= 2;
+    const int64_t heads = (int64_t)s->n_obj * s->H_kv;
+    while (TR > 4 && (TR * a->pitch * 4 > 81920 - 6144 || TR / 2 >= s->n_q || heads * ((s->n_q + TR - 1) / TR) < 256))
+      TR /= 2;
     int64_t lds = (int64_t)TR * a->pitch * 4;
     lds = std::max<int64_t>(lds, std::max<int64_t>(n_blk * 8, q_lds));
     if (lds <= SELECT_LDS) {

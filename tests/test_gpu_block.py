@@ -206,6 +206,14 @@ def test_block_select(n_obj, n_q, n_kv, H, H_kv, d_h, block, top_k, first, last,
     run_select(n_obj, n_q, n_kv, H, H_kv, d_h, block, top_k, first, last, vis, dtype, seed=n_q + n_kv)
 
 
+@pytest.mark.parametrize("n_obj,n_q,n_kv,H,H_kv,d_h,block,top_k,first,last,vis,dtype", [
+    (1, 4, 1000, 128, 128, 64, 32, 6, 1, 1, "all", "bf16"), (3, 300, 1500, 6, 1, 128, 64, 7, 0, 1, "ragged", "bf16"),
+    (1, 2100, 700, 8, 4, 64, 32, 9, 1, 2, "causal", "bf16"), (9, 517, 500, 2, 2, 256, 32, 4, 0, 0, "ragged", "f32"),
+    (33, 17, 40000, 1, 1, 32, 32, 12, 2, 0, "ragged", "bf16")])
+def test_block_select_many_queries(n_obj, n_q, n_kv, H, H_kv, d_h, block, top_k, first, last, vis, dtype):
+    run_select(n_obj, n_q, n_kv, H, H_kv, d_h, block, top_k, first, last, vis, dtype, seed=n_q + n_kv)
+
+
 def all_zero(rng, Q, M):
     return Q * 0, M
 
@@ -254,6 +262,11 @@ def tiny(rng, Q, M):
 @pytest.mark.parametrize("n_kv", [1500, 50000])
 def test_block_select_hard_scores(make, n_kv):
     run_select(2, 37, n_kv, 4, 2, 64, 32, 11, 1, 1, "ragged", "bf16", seed=n_kv, make=make)
+
+
+@pytest.mark.parametrize("make", [all_zero, equal_means, few_values, close_scores, not_finite, huge, tiny])
+def test_block_select_hard_scores_of_many_queries(make):
+    run_select(3, 150, 15000, 4, 2, 64, 32, 11, 1, 1, "ragged", "bf16", seed=5, make=make)
 
 
 def test_block_select_nothing_to_read():
@@ -365,6 +378,34 @@ def test_block_attend_lists_and_layouts(case, kw):
     check_attend(got, *args)
 
 
+# Enough rows that queries which chose a block share its keys.
+MANY = [
+    (4, 500, 600, 2, 2, 128, 64, 8, "all", "bf16"), (1, 1100, 700, 4, 4, 32, 32, 6, "causal", "bf16"),
+    (3, 450, 333, 6, 2, 64, 32, 5, "ragged", "bf16"), (1, 1029, 1300, 10, 2, 128, 128, 4, "causal", "bf16"),
+    (1, 1400, 600, 3, 1, 256, 64, 3, "causal", "bf16"), (4, 390, 1030, 7, 1, 64, 256, 3, "ragged", "bf16"),
+    (2, 1260, 50, 4, 4, 64, 32, 3, "causal", "bf16"), (2, 330, 3000, 1, 1, 256, 256, 9, "ragged", "bf16"),
+    (350, 8, 100, 2, 1, 64, 64, 2, "ragged", "bf16"), (1, 600, 1500, 64, 2, 256, 32, 32, "causal", "bf16"),
+    (1, 800, 500, 40, 2, 64, 64, 3, "ragged", "bf16"),
+    (1, 700, 600, 4, 4, 64, 32, 8, "causal", "f32"), (2, 880, 500, 5, 1, 32, 128, 3, "ragged", "f32"),
+    (2, 400, 300, 2, 2, 256, 64, 3, "causal", "f32"), (1, 500, 300, 8, 4, 128, 256, 2, "all", "f32")]
+
+
+@pytest.mark.parametrize("n_obj,n_q,n_kv,H,H_kv,d_h,block,top_k,vis,dtype", MANY)
+def test_block_attend_many_queries(n_obj, n_q, n_kv, H, H_kv, d_h, block, top_k, vis, dtype):
+    p = rs3()
+    s = p.block_shape(dt_of(dtype), n_obj, n_q, n_kv, H, H_kv, d_h, block, top_k)
+    assert p.block_attend_workspace_size(s) > 0    # so many rows of their own would need none
+    got, args = run_attend(n_obj, n_q, n_kv, H, H_kv, d_h, block, top_k, vis, dtype, seed=n_q + n_kv + d_h)
+    check_attend(got, *args)
+
+
+@pytest.mark.parametrize("case", [0, 2, 6, 11])
+@pytest.mark.parametrize("kw", [dict(wrong=True), dict(strided=True), dict(shared=True)])
+def test_block_attend_many_queries_lists_and_layouts(case, kw):
+    got, args = run_attend(*MANY[case], seed=case, **kw)
+    check_attend(got, *args)
+
+
 def unseen_garbage(rng, Q, K, V, v):
     """NaN and Inf in keys and values that nobody, or only later queries, see."""
     top = int(np.max(np.clip(v, 0, K.shape[1])))
@@ -377,7 +418,16 @@ def unseen_garbage(rng, Q, K, V, v):
 
 @pytest.mark.parametrize("case", [2, 3, 7, 8, 9, 11, 15, 16])
 def test_block_attend_masked_garbage(case):
-    c = list(ATTEND[case])
+    check_masked_garbage(ATTEND[case], case)
+
+
+@pytest.mark.parametrize("case", [1, 2, 3, 5, 8, 11, 12])
+def test_block_attend_masked_garbage_of_many_queries(case):
+    check_masked_garbage(MANY[case], case)
+
+
+def check_masked_garbage(c, case):
+    c = list(c)
     c[2] += 70
     if c[8] == "causal":
         # every query stops short of the last keys
@@ -397,13 +447,22 @@ def test_block_attend_masked_garbage(case):
 def test_block_attend_garbage_seen_by_later_queries(dtype, d_h, G):
     """A query must not meet the Inf or NaN of a key that only later queries of
     the same block see; those queries get what the formula gives, no number."""
+    check_garbage_seen_by_later_queries(1, dtype, d_h, G)
+
+
+@pytest.mark.parametrize("dtype,d_h,G", [("bf16", 64, 1), ("bf16", 128, 4), ("f32", 64, 2)])
+def test_block_attend_garbage_seen_by_later_queries_of_many(dtype, d_h, G):
+    check_garbage_seen_by_later_queries(30, dtype, d_h, G)
+
+
+def check_garbage_seen_by_later_queries(n_obj, dtype, d_h, G):
     n_q = 96
     def edit(rng, Q, K, V, v):
         V[0, 70, 0, 3] = 0x7FC0 if dtype == "bf16" else np.nan
         V[0, 80, 0, 5] = 0x7F80 if dtype == "bf16" else np.inf
         K[0, 85, 0, 7] = 0x7FC0 if dtype == "bf16" else np.nan
         return Q, K, V
-    got, args = run_attend(1, n_q, n_q, G, 1, d_h, 64, 2, "causal", dtype, seed=9, edit=edit)
+    got, args = run_attend(n_obj, n_q, n_q, G, 1, d_h, 64, 2, "causal", dtype, seed=9, edit=edit)
     Q, K, V, idx, count, v, block, _ = args
     reads = np.array([1 in B.valid_blocks(idx[0, i, 0], count[0, i, 0], 2) for i in range(n_q)])
     early = (v[0] <= 70) | ~reads
@@ -427,7 +486,7 @@ def test_block_attend_extreme_logits():
         k[:, 64:96] *= 0
         k[:, 64:96, :, 1] = -3e38                                          # overflow to -inf
         return to_storage(q.astype(np.float32), "bf16"), to_storage(k.astype(np.float32), "bf16"), V
-    for n_q in (1, 130):
+    for n_q in (1, 130, 2000):
         got, args = run_attend(1, n_q, 320, 2, 2, 64, 32, 10, "all", "bf16", seed=n_q, edit=edit)
         assert np.isfinite(got).all()
         Q, K, V, idx, count, v, block, _ = args
@@ -506,7 +565,7 @@ def test_captured_calls_replay():
     """The three calls in a graph, replayed on new inputs between eager calls."""
     p = rs3()
     n_obj, n_q, n_kv, H, H_kv, d_h, block, top_k = 1, 200, 1000, 4, 2, 64, 32, 6
-    for n_q in (1, 200):
+    for n_q in (1, 200, 2000):
         s = p.block_shape(p.RS3_BF16, n_obj, n_q, n_kv, H, H_kv, d_h, block, top_k, 1, 1)
         Q = torch.zeros((n_obj, n_q, H, d_h), dtype=torch.bfloat16, device="cuda")
         K, V = (torch.zeros((n_obj, n_kv, H_kv, d_h), dtype=torch.bfloat16, device="cuda") for _ in range(2))
