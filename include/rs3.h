@@ -516,8 +516,9 @@ rs3_status rs3_block_select(const rs3_block_shape* s /*[host]*/, const void* Q, 
 
 /* O_h = softmax(q_h K^T / sqrt(d_h)) V over the keys below n_vis of the listed
  * blocks; 0 for a row without any.  idx and count as rs3_block_select writes
- * them, or the caller's own lists: a count is taken into [0, top_k], and an
- * entry that is out of range or not above the entry before it takes no part.
+ * them, or the caller's own lists: a count is taken into [0, min(top_k,
+ * n_blk)], and an entry that is out of range or not above the entry before it
+ * takes no part.
  * Logits of -inf have weight 0.  The bf16 form rounds the weights to bf16 for
  * the matrix cores; sums are fp32, and O is rounded to `dt` once.
  * ws : at least rs3_block_attend_workspace_size() bytes */

@@ -63,8 +63,8 @@ def block_select(Q, Kmean, n_vis, block, top_k, n_first, n_last, n_kv):
 
 
 def valid_blocks(idx, count, n_blk):
-    """The entries of one list that take part."""
-    c = min(max(int(count), 0), len(idx))
+    """The entries of one list that take part (an ascending list has no more than n_blk)."""
+    c = min(max(int(count), 0), len(idx), n_blk)
     return [int(b) for t, b in enumerate(idx[:c]) if 0 <= b < n_blk and (t == 0 or b > idx[t - 1])]
 
 

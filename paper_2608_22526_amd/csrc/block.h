@@ -58,6 +58,7 @@ struct BlockAttendArgs {
   const int32_t* n_vis;
   float qscale;            // log2(e) / sqrt(d_h)
   int n_obj, n_q, n_kv, H, H_kv, G, d_h, block, n_blk, top_k;
+  int slots;               // entries of a list that can take part: min(top_k, n_blk)
 };
 
 // Blocks of keys that the counters of the tiled attention hold.
@@ -72,11 +73,11 @@ struct BlockTile {
   int b, n;                // block (-1: no tile), and how many queries
 };
 struct BlockTileArgs {
-  uint32_t* ord;           // [groups][n_q][top_k] place of an entry among its run's queries of its block,
+  uint32_t* ord;           // [groups][n_q][slots] place of an entry among its run's queries of its block,
                            //   times BLOCK_TILE_MAX, + the block; ~0: none
   uint32_t* total;         // [chunks][groups][n_blk] queries that list the block
   uint32_t* base;          // [chunks * runs][groups][n_blk] where each run's begin among them
-  uint32_t* list;          // [chunks][groups][tcap][tq] query of the chunk * top_k + slot
+  uint32_t* list;          // [chunks][groups][tcap][tq] query of the chunk * slots + slot
   BlockTile* tiles;        // [chunks][groups][tcap]
   int chunk, chunks, ch, nq;   // queries per chunk, chunks; this launch's chunk and its queries
   int run, runs;           // queries of one counting work-group, runs per chunk

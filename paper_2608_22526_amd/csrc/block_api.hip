@@ -68,13 +68,14 @@ constexpr size_t PART_BYTES = (size_t)256 << 20;   // partial rows of a chunk of
 void attend_plan(const rs3_block_shape* s, AttendPlan* a) {
   memset(a, 0, sizeof(*a));
   const int n_blk = (s->n_kv + s->block - 1) / s->block, G = s->H / s->H_kv;
+  const int slots = std::min(s->top_k, n_blk);
   size_t off = 0;
   auto take = [&](size_t bytes) {
     const size_t at = off;
     off += align256(bytes);
     return at;
   };
-  const size_t per_q = (size_t)s->n_obj * s->H * s->top_k * s->d_h * elem(s->dt);   // partial rows of one query
+  const size_t per_q = (size_t)s->n_obj * s->H * slots * s->d_h * elem(s->dt);   // partial rows of one query
   // What the row form reads: the keys and values of each row's blocks, and as much
   // time as 128 KiB more for the row itself. The tile form reads each once, but has
   // five launches and the partial rows. Against 320 MiB and twice the cache (row and
@@ -86,7 +87,7 @@ void attend_plan(const rs3_block_shape* s, AttendPlan* a) {
   //   1 x n_q, 8/8 heads of 64, fp32, 16 of 128 blocks of 32: n_q 32 12/24, 64 22/25, 128 41/27
   const int64_t rows = (int64_t)s->n_obj * s->n_q * s->H_kv * ((G + 15) / 16);
   const int64_t key_bytes = (int64_t)2 * s->d_h * elem(s->dt);
-  const int64_t keys = std::min<int64_t>((int64_t)s->top_k * s->block, s->n_kv);
+  const int64_t keys = std::min<int64_t>((int64_t)slots * s->block, s->n_kv);
   const double row_reads = (double)rows * (keys * key_bytes + (128 << 10));
   const double tile_reads = (320 << 20) + 2.0 * s->n_obj * s->H_kv * s->n_kv * key_bytes;
   a->tile = s->n_q >= 8 && row_reads > tile_reads && n_blk <= BLOCK_TILE_MAX && n_blk > 0 && per_q <= (16u << 20) &&
@@ -96,23 +97,23 @@ void attend_plan(const rs3_block_shape* s, AttendPlan* a) {
     a->chunks = (int)((s->n_q + most_q - 1) / most_q);
     a->chunk = (s->n_q + a->chunks - 1) / a->chunks;
     a->groups = s->n_obj * s->H_kv;
-    a->run = 2048 / s->top_k;
+    a->run = 2048 / slots;
     if (a->run < 64) a->run = 64;
     a->runs = (a->chunk + a->run - 1) / a->run;
     a->tq = 32 * BLOCK_TILE_WAVES / G;
-    const int64_t entries = (int64_t)a->chunk * s->top_k;
+    const int64_t entries = (int64_t)a->chunk * slots;
     a->tcap = (int)(entries / a->tq + (n_blk < entries ? n_blk : entries));
-    a->ord = take((size_t)s->n_q * s->top_k * a->groups * 4);
+    a->ord = take((size_t)s->n_q * slots * a->groups * 4);
     a->cnt = take((size_t)a->chunks * a->groups * n_blk * 4);
     a->base = take((size_t)a->chunks * a->runs * a->groups * n_blk * 4);
     a->list = take((size_t)a->chunks * a->tcap * a->groups * a->tq * 4);
     a->tiles = take((size_t)a->chunks * a->tcap * a->groups * sizeof(BlockTile));
     a->opart = take(entries * s->H * s->n_obj * s->d_h * elem(s->dt));
-    a->ml = take((size_t)s->n_q * s->top_k * s->H * s->n_obj * 8);
+    a->ml = take((size_t)s->n_q * slots * s->H * s->n_obj * 8);
   } else {
     // a work-group per CU, each with a few pieces of 32 keys per wave
     int64_t S = rows > 0 ? 256 / rows : 1;
-    const int64_t most = (int64_t)s->top_k * s->block / 32 / 8;
+    const int64_t most = (int64_t)slots * s->block / 32 / 8;
     S = S < most ? S : most;
     a->S = (int)(S < 1 ? 1 : S);
     if (a->S > 1) {
@@ -337,6 +338,7 @@ rs3_status rs3_block_attend(const rs3_block_shape* s, const void* Q, const void*
   a.block = s->block;
   a.n_blk = n_blocks(s);
   a.top_k = s->top_k;
+  a.slots = std::min(a.top_k, a.n_blk);
   const hipStream_t st = (hipStream_t)stream;
   uint8_t* w = (uint8_t*)ws;
   BlockPartArgs part;
@@ -364,7 +366,7 @@ rs3_status rs3_block_attend(const rs3_block_shape* s, const void* Q, const void*
   t.tq = pl.tq;
   t.tcap = pl.tcap;
   t.groups = pl.groups;
-  part.S = s->top_k;
+  part.S = a.slots;
   hipError_t e = rs3_launch_block_lists(a, t, part, st);
   for (t.ch = 0; t.ch < pl.chunks && e == hipSuccess; ++t.ch) {
     part.i0 = t.ch * pl.chunk;

@@ -17,11 +17,13 @@ __device__ __forceinline__ float max4(float v) {
   return max_with_partner(v);
 }
 
-// LDS of k_block_row: two stages of 32 keys and values per wave, or after the
-// products every wave's sums of 16 heads.
+// LDS of k_block_row: two stages of KP keys and values per wave, or after the
+// products every wave's sums of 16 heads.  KP is 32, the keys of one bf16 value
+// product; long fp32 rows, whose products take eight times as long, go in pieces
+// of 16 so that more waves (and their SIMDs) find room.
 template <class T, int D>
 struct RowLayout {
-  static constexpr int CPR = D * (int)sizeof(T) / 16, VOFF = 32 * CPR * 16, STAGE = 2 * VOFF, WAVE = 2 * STAGE;
+  static constexpr int CPR = D * (int)sizeof(T) / 16, KP = CPR >= 32 && sizeof(T) == 4 ? 16 : 32, VOFF = KP * CPR * 16, STAGE = 2 * VOFF, WAVE = 2 * STAGE;
   static constexpr int NW = 131072 / WAVE < 4 ? 131072 / WAVE : 4;
   static constexpr int XP = D + 4;   // floats of a head's sums
   static_assert(16 * XP * 4 + 16 * 8 <= WAVE, "the sums fit the stages");
@@ -29,7 +31,7 @@ struct RowLayout {
 
 // One work-group per (query, key head), 16 of its query heads and a split of
 // its keys.  The valid blocks of the list go to LDS; the waves take their
-// 32-key pieces in turn, each into stages of its own by direct-to-LDS loads one
+// KP-key pieces in turn, each into stages of its own by direct-to-LDS loads one
 // piece ahead, so that no barrier stands between the pieces.  The G query heads
 // of the key head are the columns of 16x16 products: S^T = K Q^T, and the
 // weights feed O^T += V^T P^T from their registers.  Keys past the last that
@@ -38,7 +40,7 @@ template <class T, int D, int NW>
 __global__ __launch_bounds__(64 * NW) void k_block_row(BlockAttendArgs p, BlockPartArgs part, int HT) {
   using L = RowLayout<T, D>;
   constexpr bool BF = sizeof(T) == 2;
-  constexpr int CPR = L::CPR, NDT = D / 16, NQ = BF ? D / 32 : D / 16;
+  constexpr int CPR = L::CPR, KP = L::KP, NKT = KP / 16, NDT = D / 16, NQ = BF ? D / 32 : D / 16;
   extern __shared__ __attribute__((aligned(1024))) uint8_t lds[];
   __shared__ int blist[256], bcount;
   const int tid = threadIdx.x, lane = tid & 63, l15 = lane & 15, g = lane >> 4;
@@ -50,7 +52,7 @@ __global__ __launch_bounds__(64 * NW) void k_block_row(BlockAttendArgs p, BlockP
   const int64_t o = oi / p.n_q, i = oi - o * p.n_q;
   const int v = visible_keys(p.n_vis, oi, p.n_kv);
   if (wave == 0) {
-    const int cnt = min(gload(p.count + row), p.top_k);
+    const int cnt = min(gload(p.count + row), p.slots);
     const int32_t* list = p.idx + row * p.top_k;
     int n = 0;
     for (int t0 = 0; t0 < cnt; t0 += 64) {
@@ -73,7 +75,7 @@ __global__ __launch_bounds__(64 * NW) void k_block_row(BlockAttendArgs p, BlockP
 #pragma unroll
   for (int k = 0; k < NQ; ++k) q[k] = head_on ? q[k] : u32x4{0, 0, 0, 0};
   __syncthreads();
-  const int upb = p.block / 32, U = bcount * upb;   // 32-key pieces
+  const int upb = p.block / KP, U = bcount * upb;   // pieces
   const int u1 = (int)((int64_t)U * (s + 1) / part.S);
   int u = (int)((int64_t)U * s / part.S) + wave;
   const T* Kg = (const T*)p.K + o * p.ko + (int64_t)hk * D;
@@ -82,7 +84,7 @@ __global__ __launch_bounds__(64 * NW) void k_block_row(BlockAttendArgs p, BlockP
   // apart) x 64 bytes
   auto fv = [](int r) { return BF ? Swz<CPR>::template v<2, 0>(r) : Swz<CPR>::template v<4, 2>(r); };
   uint8_t* mine = lds + wave * L::WAVE;
-  auto first_key = [&](int x) { return (int64_t)blist[x / upb] * p.block + x % upb * 32; };
+  auto first_key = [&](int x) { return (int64_t)blist[x / upb] * p.block + x % upb * KP; };
   // Direct-to-LDS loads: load k covers 64 chunks, rows k * RPL + r0 with r0 <
   // RPL, whose swizzles are those of r0 xor those of k * RPL.  Rows past the last
   // that the query sees read that one.
@@ -95,23 +97,23 @@ __global__ __launch_bounds__(64 * NW) void k_block_row(BlockAttendArgs p, BlockP
     uint8_t* st = mine + slot * L::STAGE;
     const uint8_t* kb = (const uint8_t*)(Kg + j0 * p.ks);
     const uint8_t* vb = (const uint8_t*)(Vg + j0 * p.vs);
-    if (j0 + 32 <= v) {
+    if (j0 + KP <= v) {
       const int ro = r0 * ksb, wo = r0 * vsb;
 #pragma unroll
-      for (int k = 0; k < CPR / 2; ++k)
+      for (int k = 0; k < CPR * KP / 64; ++k)
         dma16(kb + (int64_t)k * RPL * ksb + (ro + (xk ^ 16 * Swz<CPR>::k(k * RPL))), st + k * 1024);
 #pragma unroll
-      for (int k = 0; k < CPR / 2; ++k)
+      for (int k = 0; k < CPR * KP / 64; ++k)
         dma16(vb + (int64_t)k * RPL * vsb + (wo + (xv ^ 16 * fv(k * RPL))), st + L::VOFF + k * 1024);
     } else {
       const int64_t last = v - 1 - j0;   // below 0 where the query sees none of these keys
 #pragma unroll
-      for (int k = 0; k < CPR / 2; ++k) {
+      for (int k = 0; k < CPR * KP / 64; ++k) {
         const int64_t r = min((int64_t)(k * RPL + r0), last);
         dma16(kb + r * ksb + (xk ^ 16 * Swz<CPR>::k(k * RPL)), st + k * 1024);
       }
 #pragma unroll
-      for (int k = 0; k < CPR / 2; ++k) {
+      for (int k = 0; k < CPR * KP / 64; ++k) {
         const int64_t r = min((int64_t)(k * RPL + r0), last);
         dma16(vb + r * vsb + (xv ^ 16 * fv(k * RPL)), st + L::VOFF + k * 1024);
       }
@@ -123,18 +125,20 @@ __global__ __launch_bounds__(64 * NW) void k_block_row(BlockAttendArgs p, BlockP
   float m = -INFINITY, l = 0.f;
   if (u < u1) issue(u, 0);
   for (int slot = 0; u < u1; u += NW, slot ^= 1) {
-    const int left = (int)min(v - first_key(u), (int64_t)32);
+    const int left = (int)min(v - first_key(u), (int64_t)KP);
     if (u + NW < u1) {
       issue(u + NW, slot ^ 1);
-      wait_vmcnt<CPR < 63 ? CPR : 62>();
+      wait_vmcnt<(CPR * KP / 32 < 63 ? CPR * KP / 32 : 62)>();
     } else {
       wait_vmcnt<0>();
     }
     asm volatile("" ::: "memory");   // the stage is read after the wait
     const uint8_t* st = mine + slot * L::STAGE;
-    f32x4 sc[2] = {f32x4{0.f, 0.f, 0.f, 0.f}, f32x4{0.f, 0.f, 0.f, 0.f}};
+    f32x4 sc[NKT];
 #pragma unroll
-    for (int kt = 0; kt < 2; ++kt)
+    for (int kt = 0; kt < NKT; ++kt) sc[kt] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int kt = 0; kt < NKT; ++kt)
 #pragma unroll
       for (int k = 0; k < NQ; ++k) {
         const u32x4 a = *(const u32x4*)(st + ((16 * kt + l15) * CPR + ((4 * k + g) ^ Swz<CPR>::k(16 * kt + l15))) * 16);
@@ -146,15 +150,15 @@ __global__ __launch_bounds__(64 * NW) void k_block_row(BlockAttendArgs p, BlockP
             sc[kt] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(a[e]), __uint_as_float(q[k][e]), sc[kt], 0, 0, 0);
         }
       }
-    if (left < 32) {
+    if (left < KP) {
 #pragma unroll
-      for (int kt = 0; kt < 2; ++kt)
+      for (int kt = 0; kt < NKT; ++kt)
 #pragma unroll
         for (int r = 0; r < 4; ++r) sc[kt][r] = 16 * kt + 4 * g + r < left ? sc[kt][r] : -INFINITY;
     }
     float mx = __builtin_elementwise_maximum(max3f(sc[0][0], sc[0][1], sc[0][2]), sc[0][3]);
-    mx = max3f(mx, sc[1][0], sc[1][1]);
-    mx = max3f(mx, sc[1][2], sc[1][3]);
+#pragma unroll
+    for (int kt = 1; kt < NKT; ++kt) mx = max3f(max3f(mx, sc[kt][0], sc[kt][1]), sc[kt][2], sc[kt][3]);
     const float mn = __builtin_elementwise_maximum(m, max4(mx) * p.qscale);
     const float sub = mn == -INFINITY ? 0.f : mn;
     const float alpha = __builtin_amdgcn_exp2f(m - sub);
@@ -165,7 +169,7 @@ __global__ __launch_bounds__(64 * NW) void k_block_row(BlockAttendArgs p, BlockP
     m = mn;
     l *= alpha;
 #pragma unroll
-    for (int kt = 0; kt < 2; ++kt)
+    for (int kt = 0; kt < NKT; ++kt)
 #pragma unroll
       for (int r = 0; r < 4; ++r) sc[kt][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[kt][r], p.qscale, -sub));
     if constexpr (BF) {
@@ -186,7 +190,7 @@ __global__ __launch_bounds__(64 * NW) void k_block_row(BlockAttendArgs p, BlockP
       }
     } else {
 #pragma unroll
-      for (int kt = 0; kt < 2; ++kt)
+      for (int kt = 0; kt < NKT; ++kt)
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
           l += sc[kt][r];

@@ -33,7 +33,7 @@ __global__ __launch_bounds__(512) void k_block_count(BlockAttendArgs p, BlockTil
   extern __shared__ uint32_t sc[];
   const int grp = blockIdx.y, o = grp / p.H_kv, hk = grp - o * p.H_kv, tid = threadIdx.x;
   const int ch = blockIdx.x / w.runs, q0 = ch * w.chunk + (blockIdx.x - ch * w.runs) * w.run;
-  const int items = max(min(w.run, min((ch + 1) * w.chunk, p.n_q) - q0), 0) * p.top_k;
+  const int items = max(min(w.run, min((ch + 1) * w.chunk, p.n_q) - q0), 0) * p.slots;
   for (int b = tid; b < p.n_blk; b += 512) sc[b] = 0;
   __syncthreads();
   constexpr int U = 4;   // entries of a thread in flight
@@ -42,9 +42,9 @@ __global__ __launch_bounds__(512) void k_block_count(BlockAttendArgs p, BlockTil
     int64_t row[U];
 #pragma unroll
     for (int k = 0; k < U; ++k) {
-      const int e = min(e0 + 512 * k, items - 1), iq = e / p.top_k;
+      const int e = min(e0 + 512 * k, items - 1), iq = e / p.slots;
       const int64_t oi = (int64_t)o * p.n_q + q0 + iq;
-      t[k] = e - iq * p.top_k;
+      t[k] = e - iq * p.slots;
       row[k] = oi * p.H_kv + hk;
       const int32_t* list = p.idx + row[k] * p.top_k;
       b[k] = gload(list + t[k]);
@@ -55,19 +55,19 @@ __global__ __launch_bounds__(512) void k_block_count(BlockAttendArgs p, BlockTil
 #pragma unroll
     for (int k = 0; k < U; ++k) {
       if (e0 + 512 * k >= items) break;
-      const bool ok = t[k] < min(cnt[k], p.top_k) && b[k] >= 0 && b[k] < p.n_blk && (t[k] == 0 || b[k] > prev[k]) &&
+      const bool ok = t[k] < min(cnt[k], p.slots) && b[k] >= 0 && b[k] < p.n_blk && (t[k] == 0 || b[k] > prev[k]) &&
                       (int64_t)b[k] * p.block < vis[k];
       uint32_t at = ~0u;
       if (ok) {
         at = atomicAdd(&sc[b[k]], 1u) * BLOCK_TILE_MAX + (uint32_t)b[k];
       } else {
-        float* ml = part.ML + (row[k] * p.top_k + t[k]) * p.G * 2;
+        float* ml = part.ML + (row[k] * p.slots + t[k]) * p.G * 2;
         for (int g = 0; g < p.G; ++g) {
           ml[2 * g] = -INFINITY;
           ml[2 * g + 1] = 0.f;
         }
       }
-      w.ord[((int64_t)grp * p.n_q + q0) * p.top_k + e0 + 512 * k] = at;
+      w.ord[((int64_t)grp * p.n_q + q0) * p.slots + e0 + 512 * k] = at;
     }
   }
   __syncthreads();
@@ -95,8 +95,8 @@ __global__ __launch_bounds__(512) void k_block_scatter(BlockAttendArgs p, BlockT
     pre[b] = gload(w.base + ((int64_t)blockIdx.x * w.groups + grp) * p.n_blk + b);   // (anything, where it has none)
   }
   const int q0 = ch * w.chunk + run * w.run;
-  const int items = max(min(w.run, min((ch + 1) * w.chunk, p.n_q) - q0), 0) * p.top_k;
-  const uint32_t* ord = w.ord + ((int64_t)grp * p.n_q + q0) * p.top_k;
+  const int items = max(min(w.run, min((ch + 1) * w.chunk, p.n_q) - q0), 0) * p.slots;
+  const uint32_t* ord = w.ord + ((int64_t)grp * p.n_q + q0) * p.slots;
   uint32_t at4[4];   // in flight during the scan
 #pragma unroll
   for (int k = 0; k < 4; ++k) at4[k] = tid + 512 * k < items ? gload(ord + tid + 512 * k) : ~0u;
@@ -152,7 +152,7 @@ __global__ __launch_bounds__(512) void k_block_scatter(BlockAttendArgs p, BlockT
 #pragma unroll
     for (int k = 0; k < 4; ++k)
       if (at4[k] != ~0u)
-        list[pre[at4[k] % BLOCK_TILE_MAX] + at4[k] / BLOCK_TILE_MAX] = (uint32_t)(run * w.run * p.top_k + e0 + 512 * k);
+        list[pre[at4[k] % BLOCK_TILE_MAX] + at4[k] / BLOCK_TILE_MAX] = (uint32_t)(run * w.run * p.slots + e0 + 512 * k);
   }
 }
 
@@ -317,11 +317,11 @@ __global__ __launch_bounds__(64 * NW, D * sizeof(T) <= 256 ? (D * sizeof(T) <= 1
   const bool there = row0 + l31 < rows;
   ent = there ? ent : 0;
   const int hg = there ? (int)(lrow - e * (uint32_t)p.G) : 0;
-  const int qi = (int)(ent / (uint32_t)p.top_k), slot = (int)(ent - (uint32_t)qi * p.top_k);
+  const int qi = (int)(ent / (uint32_t)p.slots), slot = (int)(ent - (uint32_t)qi * p.slots);
   const int64_t oi = (int64_t)o * p.n_q + i0 + qi;
   const int lim = (int)min((int64_t)visible_keys(p.n_vis, oi, p.n_kv) - j0, (int64_t)p.block);
-  const int prow = (((o * w.nq + qi) * p.H_kv + hk) * p.top_k + slot) * p.G + hg;
-  float* ml = part.ML + 2 * (((oi * p.H_kv + hk) * p.top_k + slot) * p.G + hg);
+  const int prow = (((o * w.nq + qi) * p.H_kv + hk) * p.slots + slot) * p.G + hg;
+  float* ml = part.ML + 2 * (((oi * p.H_kv + hk) * p.slots + slot) * p.G + hg);
   const T* Qo = (const T*)p.Q + o * p.qo + (int64_t)i0 * p.qs + (int64_t)hk * p.G * D;
   const T* qp = Qo + qi * p.qs + hg * D;
   u32x4 q[NQ];
