@@ -2,6 +2,8 @@
 // its keys), and the merge of partial rows.
 #include "block.h"
 
+#include <type_traits>
+
 namespace rs3 {
 
 // Operand of 16 heads: the sum over the four lane groups that share a head,
@@ -260,7 +262,7 @@ __global__ __launch_bounds__(64 * NW) void k_block_row(BlockAttendArgs p, BlockP
 }
 
 // One thread per (query, head, 16 bytes of O): log-sum-exp merge of the S
-// partials, batches of 8 in flight.  F16: values and pairs as k_block_tile
+// partials, batches of 8 (the last of 4 or 1, where that holds the rest) in flight.  F16: values and pairs as k_block_tile
 // leaves them, else fp32.
 template <class T, bool F16>
 __global__ __launch_bounds__(256) void k_block_merge(BlockAttendArgs p, BlockPartArgs w) {
@@ -277,8 +279,8 @@ __global__ __launch_bounds__(256) void k_block_merge(BlockAttendArgs p, BlockPar
   float M = -INFINITY, W = 0.f, acc[CH];
 #pragma unroll
   for (int e = 0; e < CH; ++e) acc[e] = 0.f;
-  constexpr int NB = 8;
-  for (int s0 = 0; s0 < w.S; s0 += NB) {
+  auto batch = [&](auto nb, int s0) {
+    constexpr int NB = decltype(nb)::value;
     float m[NB], l[NB];
     u32x4 v[NB][F16 ? 1 : CH / 4];
     float top = M;
@@ -317,7 +319,11 @@ __global__ __launch_bounds__(256) void k_block_merge(BlockAttendArgs p, BlockPar
         for (int e = 0; e < CH; ++e) acc[e] += wt * __uint_as_float(v[k][e / 4][e % 4]);
       }
     }
-  }
+  };
+  int s0 = 0;
+  for (; s0 + 4 < w.S; s0 += 8) batch(std::integral_constant<int, 8>{}, s0);
+  if (s0 + 1 < w.S) batch(std::integral_constant<int, 4>{}, s0);
+  else if (s0 < w.S) batch(std::integral_constant<int, 1>{}, s0);
   const float inv = W == 0.f ? 0.f : 1.f / W;
   u32x4 w4;
 #pragma unroll
