@@ -40,6 +40,8 @@ struct BlockSelectArgs {
 
 // How a call of rs3_block_select runs.
 constexpr int SELECT_LDS = 131072;   // at most
+// The two terms of a tile's 32 queries.
+constexpr int select_query_lds(int d_h) { return 2 * 32 * d_h * 2; }
 struct BlockSelectPlan {
   bool tile;         // several queries of a key head per work-group, else one
   int TR, pitch;     // tile: queries, floats of a row of scores

@@ -144,14 +144,14 @@ void select_plan(const rs3_block_shape* s, BlockSelectPlan* a, size_t* ws) {
   // (256 rows of 4096 blocks 49/94). The tile: the largest whose scores leave room for
   // two work-groups per CU, smaller while that gives fewer work-groups than CUs (64
   // queries: tiles of 32 19.5, of 4 10.8), at least four queries.
-  const int q_lds = 2 * 32 * s->d_h * 2;   // the queries' two terms
+  const int q_lds = select_query_lds(s->d_h), before = s->d_h > 128 ? q_lds : 0;   // before the scores
   a->pitch = (int)((n_blk + 31) / 32 * 32 + 4);
   if (s->n_q >= 4 && (rows > 256 || (s->n_q >= 8 && n_blk <= 256))) {
     int TR = 32;
     const int64_t heads = (int64_t)s->n_obj * s->H_kv;
-    while (TR > 4 && (TR * a->pitch * 4 > 81920 - 6144 || TR / 2 >= s->n_q || heads * ((s->n_q + TR - 1) / TR) < 256))
+    while (TR > 4 && (before + TR * a->pitch * 4 > 81920 - 6144 || TR / 2 >= s->n_q || heads * ((s->n_q + TR - 1) / TR) < 256))
       TR /= 2;
-    int64_t lds = (int64_t)TR * a->pitch * 4;
+    int64_t lds = before + (int64_t)TR * a->pitch * 4;
     lds = std::max<int64_t>(lds, std::max<int64_t>(n_blk * 8, q_lds));
     if (lds <= SELECT_LDS) {
       a->tile = true;

@@ -455,9 +455,11 @@ __device__ __forceinline__ bool narrow(const float (&v)[NV], int seg, More more,
 
 // TR (32, 16, 8 or 4) queries of one (object, key head) per work-group.  LDS, in
 // turn: the queries, summed over their heads and split into two bf16 terms; the
-// scores [TR][pitch]; fp64 scores of a hard row.
+// scores [TR][pitch]; fp64 scores of a hard row.  Queries of 256 channels stay in
+// LDS in front of the scores: in registers they would leave room for one
+// work-group per CU (1693 queries of 8 heads, 135 blocks: 36 us, so 25).
 template <class T, int D>
-__global__ __launch_bounds__(64 * NWS, D <= 128 ? 4 : 2) void k_select_tile(BlockSelectArgs p, int TR, int n_tile, int pitch) {
+__global__ __launch_bounds__(64 * NWS, 4) void k_select_tile(BlockSelectArgs p, int TR, int n_tile, int pitch) {
   constexpr bool BF = sizeof(T) == 2;
   constexpr int NQ = D / 16;
   extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
@@ -521,15 +523,18 @@ __global__ __launch_bounds__(64 * NWS, D <= 128 ? 4 : 2) void k_select_tile(Bloc
   for (int m = 1; m < 64; m <<= 1) nbm = max(nbm, __shfl_xor(nbm, m, 64));
   __syncthreads();
   const bool two = !BF || G > 1;   // one bf16 head is its own first term
-  u32x4 qh[NQ], ql[NQ];
+  constexpr bool QREG = D <= 128;
+  auto query = [&](int k) { return (const u32x4*)lds + l31 * CPQ + ((2 * k + half) ^ Swz<CPQ>::k(l31)); };
+  u32x4 qh[QREG ? NQ : 1], ql[QREG ? NQ : 1];
+  if constexpr (QREG) {
 #pragma unroll
-  for (int k = 0; k < NQ; ++k) {
-    const u32x4* qt = (const u32x4*)lds + l31 * CPQ + ((2 * k + half) ^ Swz<CPQ>::k(l31));
-    qh[k] = qt[0];
-    ql[k] = two ? qt[32 * CPQ] : u32x4{0, 0, 0, 0};
+    for (int k = 0; k < NQ; ++k) {
+      qh[k] = query(k)[0];
+      ql[k] = two ? query(k)[32 * CPQ] : u32x4{0, 0, 0, 0};
+    }
+    __syncthreads();
   }
-  __syncthreads();
-  float* sc = (float*)lds;
+  float* sc = (float*)(lds + (QREG ? 0 : select_query_lds(D)));
   float k2 = 0.f;   // the largest squared norm of a mean key
   for (int bt = wave; bt * 32 < nbm; bt += NWS) {
     const T* kp = km + (int64_t)min(bt * 32 + l31, nbm - 1) * D + 8 * half;
@@ -563,9 +568,10 @@ __global__ __launch_bounds__(64 * NWS, D <= 128 ? 4 : 2) void k_select_tile(Bloc
           kk = __builtin_amdgcn_fdot2_f32_bf16(v, v, kk, false);
         }
         const int ks = k0 + k;
-        acc = mfma32(ah, qh[ks], ks == 0 ? f32x16{} : acc);
-        if (two) acc = mfma32(ah, ql[ks], acc);
-        if constexpr (!BF) acc = mfma32(al, qh[ks], acc);
+        const u32x4 hi = QREG ? qh[QREG ? ks : 0] : query(ks)[0];
+        acc = mfma32(ah, hi, ks == 0 ? f32x16{} : acc);
+        if (two) acc = mfma32(ah, QREG ? ql[QREG ? ks : 0] : query(ks)[32 * CPQ], acc);
+        if constexpr (!BF) acc = mfma32(al, hi, acc);
       }
     }
     k2 = __builtin_elementwise_maximum(k2, sum_with_partner(kk));
