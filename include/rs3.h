@@ -422,7 +422,7 @@ rs3_status rs3_attend(const void* Qh, const void* Kh, const void* Vh, int32_t n_
  * column p of the table: channels (2p, 2p+1) with RS3_PAIRS_ADJACENT (as the
  * layers' tables, see rs3_layer_set_rope) or (p, p + d_rot/2) with
  * RS3_PAIRS_HALVES; (a, b) becomes (a cos - b sin, a sin + b cos).
- * n      : rows (tokens), at most 2^24
+ * n      : rows (tokens), at most 2^24, and n * (H + H_kv) <= 2^27
  * Q, K   : [n][H][d_h] and [n][H_kv][d_h] in `dt`; row i starts at element
  *          i * q_stride (k_stride).  H = 0 (or H_kv = 0) leaves that side out
  *          (its pointers may be NULL); H + H_kv <= 1024.

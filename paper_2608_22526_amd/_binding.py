@@ -443,12 +443,20 @@ def _rows(torch, name: str, t, last: int, dtype, dev: int):
     return t.data_ptr()
 
 
+def _check_i32(*values: int):
+    """ctypes would take them modulo 2^32."""
+    for v in values:
+        if not -2 ** 31 <= v < 2 ** 31:
+            raise ValueError("%d is no 32-bit integer" % v)
+
+
 def qk_norm_rope(n: int, Q, H: int, K, H_kv: int, d_h: int, dtype: int, Qo, Ko, gain_q=None, gain_k=None,
                  eps: float = 1e-6, table=None, d_rot: int = 0, pairing: int = RS3_PAIRS_ADJACENT, pos=None,
                  q_stride: Optional[int] = None, k_stride: Optional[int] = None, qo_stride: Optional[int] = None,
                  ko_stride: Optional[int] = None, stream=None):
     """RMS norm of each head of Q [n][H][d_h] and K [n][H_kv][d_h] (None with
     0 heads) and the rotation of its first d_rot channels by table[pos]."""
+    _check_i32(n, H, H_kv, d_h, d_rot)
     torch, dev, st = _call()
     dt, f32 = torch.bfloat16 if dtype == RS3_BF16 else torch.float32, torch.float32
     wq, wk = H * d_h, H_kv * d_h
@@ -483,6 +491,7 @@ def block_shape(dtype: int, n_obj: int, n_q: int, n_kv: int, H: int, H_kv: int, 
                 n_first: int = 0, n_last: int = 0, **strides) -> BlockShape:
     """A BlockShape for packed tensors [n_obj][rows][heads][d_h]; strides
     (q_stride=, q_obj_stride=, ...) replace the packed ones."""
+    _check_i32(n_obj, n_q, n_kv, H, H_kv, d_h, block, top_k, n_first, n_last)
     s = BlockShape(n_obj, n_q, n_kv, H, H_kv, d_h, block, top_k, n_first, n_last, dtype, 0)
     for x, rows, heads in (("q", n_q, H), ("k", n_kv, H_kv), ("v", n_kv, H_kv), ("o", n_q, H)):
         row = strides.pop(x + "_stride", heads * d_h)
@@ -510,6 +519,7 @@ def _shape_dtype(torch, s: BlockShape):
 def block_means(shape: BlockShape, K, Kmean, kv_len=None, n_new: int = 0, stream=None):
     """Kmean [n_obj][H_kv][n_blk][d_h]: the mean key of every block of K, or
     (n_new > 0) of the blocks that hold each object's last n_new keys."""
+    _check_i32(n_new)
     torch, dev, st = _call()
     s, dt = shape, _shape_dtype(torch, shape)
     k = _rows(torch, "K", K, _span(s.n_obj, s.k_obj_stride, s.n_kv, s.k_stride, s.H_kv * s.d_h), dt, dev)

@@ -95,6 +95,14 @@ struct BlockPartArgs {
   int S, i0, nq;
 };
 
+// Grids of many work-groups fold into two dimensions: one holds fewer than 2^32
+// threads.
+inline dim3 folded(int64_t n, unsigned z = 1) {
+  const int64_t x = std::min<int64_t>(n, 1 << 20);
+  return dim3((unsigned)x, (unsigned)((n + x - 1) / x), z);
+}
+__device__ __forceinline__ int64_t folded_block() { return (int64_t)blockIdx.y * gridDim.x + blockIdx.x; }
+
 // How many keys query `i` (of all objects' queries) sees.
 __device__ __forceinline__ int visible_keys(const int32_t* n_vis, int64_t i, int n_kv) {
   return n_vis ? min(max(gload(n_vis + i), 0), n_kv) : n_kv;

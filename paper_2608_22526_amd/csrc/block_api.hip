@@ -3,6 +3,8 @@
 #include <math.h>
 #include <string.h>
 
+#include <atomic>
+
 #include "block.h"
 
 using namespace rs3;
@@ -103,6 +105,12 @@ void attend_plan(const rs3_block_shape* s, AttendPlan* a) {
     a->tq = 32 * BLOCK_TILE_WAVES / G;
     const int64_t entries = (int64_t)a->chunk * slots;
     a->tcap = (int)(entries / a->tq + (n_blk < entries ? n_blk : entries));
+    // what the launches' grids hold
+    a->tile = (int64_t)a->runs * a->chunks <= 65535 && (int64_t)a->chunks * a->groups * n_blk < (1ll << 31) &&
+              (int64_t)a->groups * a->tcap < (1 << 23);
+  }
+  if (a->tile) {
+    const int64_t entries = (int64_t)a->chunk * slots;
     a->ord = take((size_t)s->n_q * slots * a->groups * 4);
     a->cnt = take((size_t)a->chunks * a->groups * n_blk * 4);
     a->base = take((size_t)a->chunks * a->runs * a->groups * n_blk * 4);
@@ -124,12 +132,15 @@ void attend_plan(const rs3_block_shape* s, AttendPlan* a) {
   a->total = off;
 }
 
-bool setup_done = false;
+std::atomic<uint64_t> setup_done{0};   // one bit per device
 
 rs3_status ensure_setup() {
-  if (setup_done) return RS3_OK;
+  int dev = 0;
+  if (hipGetDevice(&dev) != hipSuccess) return RS3_E_DEVICE;
+  const uint64_t bit = dev < 64 ? 1ull << dev : 0;
+  if (setup_done.load(std::memory_order_acquire) & bit) return RS3_OK;
   if (rs3_block_setup() != hipSuccess) return RS3_E_DEVICE;
-  setup_done = true;
+  setup_done.fetch_or(bit, std::memory_order_release);
   return RS3_OK;
 }
 
@@ -179,7 +190,7 @@ rs3_status rs3_qk_norm_rope(int32_t n, const void* Q, int64_t q_stride, int32_t 
                             const int32_t* pos, void* Qo, int64_t qo_stride, void* Ko, int64_t ko_stride,
                             void* stream) {
   if (n < 0 || n > (1 << 24) || (dt != RS3_BF16 && dt != RS3_F32)) return RS3_E_INVALID;
-  if (H < 0 || H_kv < 0 || H > 1024 || H_kv > 1024 - H || d_h < 16 || d_h > 256 || d_h % 16 != 0) return RS3_E_INVALID;
+  if (H < 0 || H_kv < 0 || H > 1024 || H_kv > 1024 - H || (int64_t)n * (H + H_kv) > (1 << 27) || d_h < 16 || d_h > 256 || d_h % 16 != 0) return RS3_E_INVALID;
   if (!(eps > 0.f) || !isfinite(eps)) return RS3_E_INVALID;
   if (d_rot < 0 || d_rot > d_h || d_rot % 16 != 0 || (d_rot > 0) != (table != nullptr)) return RS3_E_INVALID;
   if (pairing != RS3_PAIRS_ADJACENT && pairing != RS3_PAIRS_HALVES) return RS3_E_INVALID;

@@ -47,9 +47,10 @@ __global__ __launch_bounds__(64 * NW) void k_block_row(BlockAttendArgs p, BlockP
   __shared__ int blist[256], bcount;
   const int tid = threadIdx.x, lane = tid & 63, l15 = lane & 15, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int64_t bid = blockIdx.x;
+  const int64_t bid = folded_block();
   const int ht = (int)(bid % HT), s = (int)(bid / HT % part.S);
   const int64_t row = bid / HT / part.S, oi = row / p.H_kv;
+  if (oi >= (int64_t)p.n_obj * p.n_q) return;
   const int hk = (int)(row - oi * p.H_kv);
   const int64_t o = oi / p.n_q, i = oi - o * p.n_q;
   const int v = visible_keys(p.n_vis, oi, p.n_kv);
@@ -338,7 +339,7 @@ template <class T, int D>
 hipError_t launch_row(const BlockAttendArgs& a, const BlockPartArgs& w, hipStream_t st) {
   const int HT = (a.G + 15) / 16;
   const int64_t n = (int64_t)a.n_obj * a.n_q * a.H_kv * w.S * HT;
-  RS3_LAUNCH(RS3_K_BLOCK_ATTEND, st, (k_block_row<T, D, RowLayout<T, D>::NW>), dim3((unsigned)n), dim3(64 * RowLayout<T, D>::NW),
+  RS3_LAUNCH(RS3_K_BLOCK_ATTEND, st, (k_block_row<T, D, RowLayout<T, D>::NW>), folded(n), dim3(64 * RowLayout<T, D>::NW),
              (RowLayout<T, D>::NW * RowLayout<T, D>::WAVE), st, a, w, HT);
   return hipGetLastError();
 }

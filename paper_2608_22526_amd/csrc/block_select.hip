@@ -384,10 +384,11 @@ template <class T, int D, bool SPLIT>
 __global__ __launch_bounds__(64 * NWR) void k_select_row(BlockSelectArgs p, int per) {
   extern __shared__ double sc[];
   __shared__ PickLds<NWR> sh;
-  const int64_t row = blockIdx.x, oi = row / p.H_kv;
+  const int64_t row = folded_block(), oi = row / p.H_kv;
+  if (row >= p.rows) return;
   const int g = (int)(row - oi * p.H_kv);
   const RowRange r = row_range(p, oi);
-  const int a = max(SPLIT ? (int)blockIdx.y * per : 0, r.f_lo), b = min(SPLIT ? (int)(blockIdx.y + 1) * per : r.nb, r.last0);
+  const int a = max(SPLIT ? (int)blockIdx.z * per : 0, r.f_lo), b = min(SPLIT ? (int)(blockIdx.z + 1) * per : r.nb, r.last0);
   double* out = SPLIT ? p.score + row * p.n_blk : sc;
   if (r.want > 0 && a < b) score_row<T, D, NWR>(p, query_of<T>(p, oi, g, D), means_of<T>(p, oi, g, D), a, b, out);
   if constexpr (!SPLIT) {
@@ -399,7 +400,8 @@ __global__ __launch_bounds__(64 * NWR) void k_select_row(BlockSelectArgs p, int 
 // The lists from scores in the workspace.
 __global__ __launch_bounds__(64 * NWR) void k_select_pick(BlockSelectArgs p) {
   __shared__ PickLds<NWR> sh;
-  const int64_t row = blockIdx.x;
+  const int64_t row = folded_block();
+  if (row >= p.rows) return;
   pick_row<NWR>(p.score + row * p.n_blk, row_range(p, row / p.H_kv), p.top_k, p.idx + row * p.top_k, p.count + row, sh);
 }
 
@@ -469,8 +471,9 @@ __global__ __launch_bounds__(64 * NWS, 4) void k_select_tile(BlockSelectArgs p, 
   __shared__ u32x2 few[NWS][64];
   const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5, l31 = lane & 31;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int64_t og = blockIdx.x / n_tile;
-  const int q0 = (int)(blockIdx.x - og * n_tile) * TR, G = p.H / p.H_kv;
+  const int64_t bid = folded_block(), og = bid / n_tile;
+  if (og >= (int64_t)p.n_obj * p.H_kv) return;
+  const int q0 = (int)(bid - og * n_tile) * TR, G = p.H / p.H_kv;
   const int64_t o = og / p.H_kv;
   const int g = (int)(og - o * p.H_kv), nr = min(TR, p.n_q - q0);
   const T* qbase = (const T*)p.Q + o * p.qo + (int64_t)q0 * p.qs + (int64_t)g * G * D;
@@ -823,14 +826,14 @@ hipError_t launch(const BlockSelectArgs& a, const BlockSelectPlan& pl, hipStream
   if (pl.tile) {
     const int n_tile = (a.n_q + pl.TR - 1) / pl.TR;
     const int64_t n = (int64_t)a.n_obj * a.H_kv * n_tile;
-    RS3_LAUNCH(RS3_K_BLOCK_SELECT, st, (k_select_tile<T, D>), dim3((unsigned)n), dim3(64 * NWS), pl.lds, st, a, pl.TR,
+    RS3_LAUNCH(RS3_K_BLOCK_SELECT, st, (k_select_tile<T, D>), folded(n), dim3(64 * NWS), pl.lds, st, a, pl.TR,
                n_tile, pl.pitch);
   } else if (pl.split > 1) {
-    RS3_LAUNCH(RS3_K_BLOCK_SELECT, st, (k_select_row<T, D, true>), dim3((unsigned)a.rows, pl.split), dim3(64 * NWR), 0, st,
+    RS3_LAUNCH(RS3_K_BLOCK_SELECT, st, (k_select_row<T, D, true>), folded(a.rows, pl.split), dim3(64 * NWR), 0, st,
                a, (a.n_blk + pl.split - 1) / pl.split);
-    RS3_LAUNCH(RS3_K_BLOCK_SELECT, st, k_select_pick, dim3((unsigned)a.rows), dim3(64 * NWR), 0, st, a);
+    RS3_LAUNCH(RS3_K_BLOCK_SELECT, st, k_select_pick, folded(a.rows), dim3(64 * NWR), 0, st, a);
   } else {
-    RS3_LAUNCH(RS3_K_BLOCK_SELECT, st, (k_select_row<T, D, false>), dim3((unsigned)a.rows), dim3(64 * NWR), pl.lds, st, a,
+    RS3_LAUNCH(RS3_K_BLOCK_SELECT, st, (k_select_row<T, D, false>), folded(a.rows), dim3(64 * NWR), pl.lds, st, a,
                a.n_blk);
   }
   return hipGetLastError();

@@ -26,13 +26,13 @@ __global__ __launch_bounds__(256) void k_block_zero(uint32_t* total, int64_t n) 
   if (i < n) total[i] = 0;
 }
 
-// grid (runs of all chunks, groups), 512 threads, n_blk counters in LDS.  Entries
+// grid (groups, runs of all chunks), 512 threads, n_blk counters in LDS.  Entries
 // that take no part (out of range, not ascending, past the count, not seen) get
 // no place and an empty partial.
 __global__ __launch_bounds__(512) void k_block_count(BlockAttendArgs p, BlockTileArgs w, BlockPartArgs part) {
   extern __shared__ uint32_t sc[];
-  const int grp = blockIdx.y, o = grp / p.H_kv, hk = grp - o * p.H_kv, tid = threadIdx.x;
-  const int ch = blockIdx.x / w.runs, q0 = ch * w.chunk + (blockIdx.x - ch * w.runs) * w.run;
+  const int grp = blockIdx.x, o = grp / p.H_kv, hk = grp - o * p.H_kv, tid = threadIdx.x;
+  const int ch = blockIdx.y / w.runs, q0 = ch * w.chunk + (blockIdx.y - ch * w.runs) * w.run;
   const int items = max(min(w.run, min((ch + 1) * w.chunk, p.n_q) - q0), 0) * p.slots;
   for (int b = tid; b < p.n_blk; b += 512) sc[b] = 0;
   __syncthreads();
@@ -74,7 +74,7 @@ __global__ __launch_bounds__(512) void k_block_count(BlockAttendArgs p, BlockTil
   // the run's place among the chunk's: in the order in which the runs come by,
   // which decides where a row is computed and nothing else
   uint32_t* total = w.total + ((int64_t)ch * w.groups + grp) * p.n_blk;
-  uint32_t* base = w.base + ((int64_t)blockIdx.x * w.groups + grp) * p.n_blk;
+  uint32_t* base = w.base + ((int64_t)blockIdx.y * w.groups + grp) * p.n_blk;
   for (int b = tid; b < p.n_blk; b += 512)
     if (sc[b]) base[b] = atomicAdd(total + b, sc[b]);
 }
@@ -87,12 +87,12 @@ __global__ __launch_bounds__(512) void k_block_scatter(BlockAttendArgs p, BlockT
   __shared__ uint32_t wsum[8], ntile;
   uint32_t* pre = sm;
   uint32_t* tot = sm + p.n_blk;
-  const int ch = blockIdx.x / w.runs, run = blockIdx.x - ch * w.runs, grp = blockIdx.y;
+  const int ch = blockIdx.y / w.runs, run = blockIdx.y - ch * w.runs, grp = blockIdx.x;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int64_t cg = (int64_t)ch * w.groups + grp;
   for (int b = tid; b < p.n_blk; b += 512) {
     tot[b] = gload(w.total + cg * p.n_blk + b);
-    pre[b] = gload(w.base + ((int64_t)blockIdx.x * w.groups + grp) * p.n_blk + b);   // (anything, where it has none)
+    pre[b] = gload(w.base + ((int64_t)blockIdx.y * w.groups + grp) * p.n_blk + b);   // (anything, where it has none)
   }
   const int q0 = ch * w.chunk + run * w.run;
   const int items = max(min(w.run, min((ch + 1) * w.chunk, p.n_q) - q0), 0) * p.slots;
@@ -546,7 +546,7 @@ using namespace rs3;
 
 hipError_t rs3_launch_block_lists(const BlockAttendArgs& a, const BlockTileArgs& t, const BlockPartArgs& w,
                                   hipStream_t st) {
-  const dim3 grid(t.runs * t.chunks, t.groups);
+  const dim3 grid(t.groups, t.runs * t.chunks);
   const int64_t n = (int64_t)t.chunks * t.groups * a.n_blk;
   RS3_LAUNCH(RS3_K_BLOCK_ATTEND, st, k_block_zero, dim3((unsigned)((n + 255) / 256)), dim3(256), 0, st, t.total, n);
   RS3_LAUNCH(RS3_K_BLOCK_ATTEND, st, k_block_count, grid, dim3(512), a.n_blk * 4, st, a, t, w);

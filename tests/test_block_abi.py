@@ -161,3 +161,19 @@ def test_binding_refuses_tensors():
             b._check_rows("t", *args)
     with pytest.raises(TypeError):
         b.block_shape(b.RS3_BF16, 1, 1, 1, 1, 1, 32, 32, 1, x_stride=3)
+
+
+def test_binding_refuses_integers_past_32_bits(p):
+    with pytest.raises(ValueError):
+        p.block_shape(p.RS3_BF16, 1, 1, 2 ** 32 + 5, 1, 1, 32, 32, 1)
+    with pytest.raises(ValueError):
+        p.block_means(shape(p), None, None, n_new=2 ** 32)
+    with pytest.raises(ValueError):
+        p.qk_norm_rope(2 ** 32, None, 0, None, 0, 64, p.RS3_BF16, None, None)
+
+
+def test_norm_refuses_more_heads_than_a_launch_holds(p):
+    n = 1 << 24
+    wide = dict(n=n, n_pos=n, qs=1024, ks=1024, qos=1024, kos=1024)
+    assert norm(p, **wide, H=7, Hk=2) == p.RS3_E_INVALID
+    assert norm(p, **wide, H=9, Hk=0) == p.RS3_E_INVALID

@@ -499,6 +499,49 @@ def test_block_attend_extreme_logits():
         check_attend(got, Q, Kc, V, idx, count, v, block, "bf16")
 
 
+@pytest.mark.parametrize("n_q,H,H_kv,n_kv,top_k,dtype", [(3, 128, 128, 64, 1, "bf16"), (33, 256, 256, 40, 1, "bf16"),
+                                                         (8, 17, 17, 40, 2, "f32")])
+def test_more_rows_than_one_grid_dimension(n_q, H, H_kv, n_kv, top_k, dtype):
+    """4096 objects at once (over 2^20 rows, over 65536 caches) against the same
+    calls for 1024 of them at a time.  Rows may be computed by other means for
+    fewer objects: each of the two lies within the bound of check_attend, whose
+    sum of the weights times |V| is the call's own result for |V| here (2 % for
+    that result's error) and whose logits are bounded by Cauchy's inequality."""
+    p = rs3()
+    gen = torch.Generator(device="cuda").manual_seed(n_q)
+    n_obj, part, d_h, block = 4096, 1024, 32, 32
+    dt = torch.bfloat16 if dtype == "bf16" else torch.float32
+    nb = -(-n_kv // block)
+    Q = torch.randn((n_obj, n_q, H, d_h), generator=gen, device="cuda", dtype=dt)
+    M = torch.randn((n_obj, H_kv, nb, d_h), generator=gen, device="cuda", dtype=dt)
+    K, V = (torch.randn((n_kv, H_kv, d_h), generator=gen, device="cuda", dtype=dt) for _ in range(2))
+
+    norm = lambda x: float(x.float().pow(2).sum(-1).max()) ** 0.5  # noqa: E731
+    delta = ((d_h + 4) * 2.0 ** -24 + 2.0 ** -22) * (norm(Q) * norm(K) / d_h ** 0.5 + 1)
+    unit = 2 * delta + n_kv * 2.0 ** -24 + (2.0 ** -7 + 2.0 ** -11 if dtype == "bf16" else 0.0)
+
+    def run(o, n, V):
+        s = p.block_shape(dt_of(dtype), n, n_q, n_kv, H, H_kv, d_h, block, top_k, k_obj_stride=0, v_obj_stride=0)
+        idx = torch.full((n, n_q, H_kv, top_k), 77, dtype=torch.int32, device="cuda")
+        count = torch.full((n, n_q, H_kv), 77, dtype=torch.int32, device="cuda")
+        O = torch.full((n, n_q, H, d_h), float("nan"), dtype=dt, device="cuda")
+        ws = torch.empty(max(p.block_select_workspace_size(s), p.block_attend_workspace_size(s), 16), dtype=torch.uint8,
+                         device="cuda")
+        p.block_select(s, Q[o:o + n], M[o:o + n], idx, count, ws=ws)
+        p.block_attend(s, Q[o:o + n], K, V, idx, count, O, ws=ws)
+        torch.cuda.synchronize()
+        return idx, count, O
+
+    (idx, count, O), A = run(0, n_obj, V), run(0, n_obj, V.abs())[2]
+    assert torch.isfinite(O).all()
+    for o in range(0, n_obj, part):
+        own = slice(o, o + part)
+        i1, c1, O1 = run(o, part, V)
+        assert torch.equal(idx[own], i1) and torch.equal(count[own], c1)
+        tol = 2 * (1.02 * unit * A[own].float() + U[dtype] * O[own].float().abs()) + 1e-30
+        assert ((O[own].float() - O1.float()).abs() <= tol).all(), o
+
+
 # ---- together --------------------------------------------------------------------
 def test_run_of_all_calls_on_a_growing_cache():
     """Norm and rotation into the cache, the newest block's mean, the choice and
