@@ -61,11 +61,12 @@ size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
 struct AttendPlan {
   bool tile;         // tiled form
   int S;             // splits of a row's keys (other form)
+  int objs;          // objects at a time
   int groups, chunk, chunks, run, runs, tq, tcap;
   size_t ord, cnt, base, list, tiles, opart, ml, total;
 };
 
-constexpr size_t PART_BYTES = (size_t)256 << 20;   // partial rows of a chunk of queries
+constexpr size_t PART_BYTES = (size_t)256 << 20;   // partial rows of a chunk of queries, or of several objects'
 
 void attend_plan(const rs3_block_shape* s, AttendPlan* a) {
   memset(a, 0, sizeof(*a));
@@ -77,7 +78,7 @@ void attend_plan(const rs3_block_shape* s, AttendPlan* a) {
     off += align256(bytes);
     return at;
   };
-  const size_t per_q = (size_t)s->n_obj * s->H * slots * s->d_h * elem(s->dt);   // partial rows of one query
+  const size_t per_q = (size_t)s->H * slots * s->d_h * elem(s->dt);   // partial rows of one query of an object
   // What the row form reads: the keys and values of each row's blocks, and as much
   // time as 128 KiB more for the row itself. The tile form reads each once, but has
   // five launches and the partial rows. Against 320 MiB and twice the cache (row and
@@ -95,10 +96,14 @@ void attend_plan(const rs3_block_shape* s, AttendPlan* a) {
   a->tile = s->n_q >= 8 && row_reads > tile_reads && n_blk <= BLOCK_TILE_MAX && n_blk > 0 && per_q <= (16u << 20) &&
             G <= 32 * BLOCK_TILE_WAVES;
   if (a->tile) {
-    const int64_t most_q = std::min<int64_t>(1 << 20, std::max<int64_t>(64, (int64_t)(PART_BYTES / per_q)));
+    // as many whole objects as PART_BYTES hold, or one and a chunk of its queries
+    const int64_t most_o = std::max<int64_t>(1, (int64_t)(PART_BYTES / (per_q * s->n_q)));
+    const int parts = (int)((s->n_obj + most_o - 1) / most_o);
+    a->objs = (s->n_obj + parts - 1) / parts;
+    const int64_t most_q = std::max<int64_t>(64, (int64_t)(PART_BYTES / (per_q * a->objs)));
     a->chunks = (int)((s->n_q + most_q - 1) / most_q);
     a->chunk = (s->n_q + a->chunks - 1) / a->chunks;
-    a->groups = s->n_obj * s->H_kv;
+    a->groups = a->objs * s->H_kv;
     a->run = 2048 / slots;
     if (a->run < 64) a->run = 64;
     a->runs = (a->chunk + a->run - 1) / a->run;
@@ -116,8 +121,8 @@ void attend_plan(const rs3_block_shape* s, AttendPlan* a) {
     a->base = take((size_t)a->chunks * a->runs * a->groups * n_blk * 4);
     a->list = take((size_t)a->chunks * a->tcap * a->groups * a->tq * 4);
     a->tiles = take((size_t)a->chunks * a->tcap * a->groups * sizeof(BlockTile));
-    a->opart = take(entries * s->H * s->n_obj * s->d_h * elem(s->dt));
-    a->ml = take((size_t)s->n_q * slots * s->H * s->n_obj * 8);
+    a->opart = take(entries * s->H * a->objs * s->d_h * elem(s->dt));
+    a->ml = take((size_t)s->n_q * slots * s->H * a->objs * 8);
   } else {
     // a work-group per CU, each with a few pieces of 32 keys per wave
     int64_t S = rows > 0 ? 256 / rows : 1;
@@ -376,14 +381,26 @@ rs3_status rs3_block_attend(const rs3_block_shape* s, const void* Q, const void*
   t.runs = pl.runs;
   t.tq = pl.tq;
   t.tcap = pl.tcap;
-  t.groups = pl.groups;
   part.S = a.slots;
-  hipError_t e = rs3_launch_block_lists(a, t, part, st);
-  for (t.ch = 0; t.ch < pl.chunks && e == hipSuccess; ++t.ch) {
-    part.i0 = t.ch * pl.chunk;
-    part.nq = t.nq = std::min(pl.chunk, s->n_q - part.i0);
-    e = rs3_launch_block_tile(a, t, part, s->dt, st);
-    if (e == hipSuccess) e = rs3_launch_block_merge(a, part, s->dt, true, st);
+  hipError_t e = hipSuccess;
+  for (int64_t o = 0; o < s->n_obj && e == hipSuccess; o += pl.objs) {
+    const int64_t es = (int64_t)elem(s->dt), rows = o * s->n_q, lists = rows * s->H_kv;
+    a.n_obj = (int)std::min<int64_t>(pl.objs, s->n_obj - o);
+    t.groups = a.n_obj * s->H_kv;
+    a.Q = (const uint8_t*)Q + o * s->q_obj_stride * es;
+    a.K = (const uint8_t*)K + o * s->k_obj_stride * es;
+    a.V = (const uint8_t*)V + o * s->v_obj_stride * es;
+    a.O = (uint8_t*)O + o * s->o_obj_stride * es;
+    a.idx = idx + lists * s->top_k;
+    a.count = count + lists;
+    a.n_vis = n_vis ? n_vis + rows : nullptr;
+    e = rs3_launch_block_lists(a, t, part, st);
+    for (t.ch = 0; t.ch < pl.chunks && e == hipSuccess; ++t.ch) {
+      part.i0 = t.ch * pl.chunk;
+      part.nq = t.nq = std::min(pl.chunk, s->n_q - part.i0);
+      e = rs3_launch_block_tile(a, t, part, s->dt, st);
+      if (e == hipSuccess) e = rs3_launch_block_merge(a, part, s->dt, true, st);
+    }
   }
   return map_err(e);
 }

@@ -387,7 +387,8 @@ MANY = [
     (350, 8, 100, 2, 1, 64, 64, 2, "ragged", "bf16"), (1, 600, 1500, 64, 2, 256, 32, 32, "causal", "bf16"),
     (1, 800, 500, 40, 2, 64, 64, 3, "ragged", "bf16"),
     (1, 700, 600, 4, 4, 64, 32, 8, "causal", "f32"), (2, 880, 500, 5, 1, 32, 128, 3, "ragged", "f32"),
-    (2, 400, 300, 2, 2, 256, 64, 3, "causal", "f32"), (1, 500, 300, 8, 4, 128, 256, 2, "all", "f32")]
+    (2, 400, 300, 2, 2, 256, 64, 3, "causal", "f32"), (1, 500, 300, 8, 4, 128, 256, 2, "all", "f32"),
+    (26, 40, 700, 64, 2, 256, 32, 16, "ragged", "bf16")]
 
 
 @pytest.mark.parametrize("n_obj,n_q,n_kv,H,H_kv,d_h,block,top_k,vis,dtype", MANY)
@@ -399,7 +400,7 @@ def test_block_attend_many_queries(n_obj, n_q, n_kv, H, H_kv, d_h, block, top_k,
     check_attend(got, *args)
 
 
-@pytest.mark.parametrize("case", [0, 2, 6, 11])
+@pytest.mark.parametrize("case", [0, 2, 6, 11, 15])
 @pytest.mark.parametrize("kw", [dict(wrong=True), dict(strided=True), dict(shared=True)])
 def test_block_attend_many_queries_lists_and_layouts(case, kw):
     got, args = run_attend(*MANY[case], seed=case, **kw)
