@@ -66,7 +66,11 @@ struct AttendPlan {
   size_t ord, cnt, base, list, tiles, opart, ml, total;
 };
 
-constexpr size_t PART_BYTES = (size_t)256 << 20;   // partial rows of a chunk of queries, or of several objects'
+// Partial rows of a chunk of queries, or of several objects': as much as the
+// memory-side cache holds until they are merged.  8192 queries, 16 heads of 128, 16
+// blocks each (537 MB, us): two chunks 2 x (108 + 51), one 230 + 148, three 3 x (87 +
+// 31).
+constexpr size_t PART_BYTES = (size_t)256 << 20;
 
 void attend_plan(const rs3_block_shape* s, AttendPlan* a) {
   memset(a, 0, sizeof(*a));
@@ -124,7 +128,9 @@ void attend_plan(const rs3_block_shape* s, AttendPlan* a) {
     a->opart = take(entries * s->H * a->objs * s->d_h * elem(s->dt));
     a->ml = take((size_t)s->n_q * slots * s->H * a->objs * 8);
   } else {
-    // a work-group per CU, each with a few pieces of 32 keys per wave
+    // a work-group per CU, each with a few pieces of 32 keys per wave (whole rows and
+    // splits in us, 8 key heads of 128: one row of 64 of 2048 blocks 31/14, four rows
+    // of 32 blocks 22/14, twelve 25/24; two or four splits of 256 rows 50/58/65)
     int64_t S = rows > 0 ? 256 / rows : 1;
     const int64_t most = (int64_t)slots * s->block / 32 / 8;
     S = S < most ? S : most;
@@ -177,7 +183,8 @@ void select_plan(const rs3_block_shape* s, BlockSelectPlan* a, size_t* ws) {
     }
   }
   // One query per work-group: its blocks over several where there are few rows
-  // or the scores do not fit the LDS.
+  // (whole rows and splits in us, 8 key heads of 128: one query of 2048 blocks 21/13,
+  // four of 1024 14.7/13.4, twelve 14.9/14.6) or the scores do not fit the LDS.
   int64_t split = rows > 0 && rows < 128 ? std::min<int64_t>(256 / rows, n_blk / 128) : 1;
   if (n_blk * 8 > SELECT_LDS) split = std::max<int64_t>(split, (n_blk + 4095) / 4096);
   a->split = (int)(split < 1 ? 1 : split);

@@ -11,13 +11,23 @@
 // keys of 128 channels and one query head); here a block is read once per 128
 // rows, and what moves is a row of Q and a partial row for every (query, head,
 // listed block).
+//
+// 4096 queries, two heads of 128, 32 of 448 blocks of 64 keys in 55 us: counters 4,
+// lists 5 + 6, tiles 29 (262144 rows, 0.3 PFLOP/s), merge 15 (67 MB, 4.5 TB/s); all
+// pairs of these queries and keys take the dense kernel 125.  8192 prompt tokens, 16
+// heads of 128 to 4 key heads, 16 of up to 512 blocks in 320: tiles 2 x 108, merge 2 x
+// 51.  The tiles are bound by the vector memory path (busy 74 % of the time): a row
+// moves 256 bytes of Q, 256 of its partial and its share of 256 of the keys and values.
 #include "block.h"
 
 namespace rs3 {
 
 typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
 
-
+// Consecutive tiles of one XCD (mostly of one block, so that its L2 serves them).
+// Runs of 8 spread a chunk's long and short lists better than an eighth of the tiles
+// for each XCD: tiles of the prompt, grid and fp32 grid 112/28.8/16.9 us against
+// 114/30.5/18.9.
 constexpr int XCD_RUN = 8;
 
 // The blocks' counters to 0 (a kernel, which a graph can hold).
@@ -245,7 +255,11 @@ struct TileLayout {
 // NW waves of 32 rows; NT 32-key tiles per stage; ONE: the block is one stage.
 // Logits transposed, S^T = K Q^T, so that the weights feed O^T += V^T P^T from
 // their registers (in bf16 the value operand comes from the rows of V by
-// transposed LDS reads); a row of the partial is one lane pair.
+// transposed LDS reads); a row of the partial is one lane pair.  In bf16 the weights
+// are rounded for the products and summed as rounded, and partials are f16 times a
+// power of two of the row's own: 2^-11 of their largest values at most, an eighth of
+// what O's rounding to bf16 takes.  They are stored past the caches (4096 queries, 32
+// blocks each, with the merge's reads: 70 us, so 59).
 template <class T, int D, int NT, int NW, bool ONE>
 __global__ __launch_bounds__(64 * NW, D * sizeof(T) <= 256 ? (D * sizeof(T) <= 128 || ONE ? 4 : 3) : 1) void k_block_tile(
     BlockAttendArgs p, BlockTileArgs w, BlockPartArgs part) {
@@ -253,7 +267,7 @@ __global__ __launch_bounds__(64 * NW, D * sizeof(T) <= 256 ? (D * sizeof(T) <= 1
   constexpr bool BF = sizeof(T) == 2;
   constexpr int CPR = L::CPR, NDT = D / 32, NQ = BF ? D / 16 : D / 8, TH = 64 * NW;
   extern __shared__ __attribute__((aligned(1024))) uint8_t lds[];
-  // XCD_RUN consecutive tiles, mostly of one block, go to one XCD and its L2
+  // XCD_RUN consecutive tiles go to one XCD
   const int64_t n_item = (int64_t)w.groups * w.tcap;
   const int turn = blockIdx.x >> 3;
   const int64_t it = ((int64_t)(turn / XCD_RUN) * 8 + (blockIdx.x & 7)) * XCD_RUN + turn % XCD_RUN;

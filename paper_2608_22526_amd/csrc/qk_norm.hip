@@ -23,7 +23,9 @@ __device__ __forceinline__ float group_sum(float v) {
 // every one: the heads are in flight together and share the row's factors, which
 // are as many bytes as four bf16 heads.  The sum of squares is a reduction over
 // the group; adjacent pairs lie in one lane, the pairs of the halves in two lanes
-// d_rot/2 channels apart.  Bound by the read and write of the tensors.
+// d_rot/2 channels apart.  Bound by the read and write of the tensors: 16384 rows
+// of 32 + 8 heads of 128 in bf16, a tenth of them padding, 344 MB in 61 us (5.6 TB/s);
+// 16384 rows of 8 + 8 heads of 32, 36 MB in 9.
 template <class T, int LPH, int HC>
 __global__ __launch_bounds__(256) void k_qk_norm(QkNormArgs p) {
   constexpr int EPL = 16 / sizeof(T), GPW = 256 / LPH;
@@ -146,12 +148,14 @@ hipError_t launch(QkNormArgs a, hipStream_t st) {
   return hipGetLastError();
 }
 
-// Four heads per group where that leaves eight waves for every SIMD, else one:
-// a few rows are a matter of latency.
+// Four heads per group where that leaves two waves for every SIMD, else one: a few
+// rows are a matter of latency.  One and four heads in us, 32/8 heads of 128: 64
+// rows 9.4/9.9, 1024 10.0/9.8, 2048 15.7/11.1, 4096 26/17.5, 16384 111/62 (two heads
+// 71, eight 65).
 template <class T, int LPH>
 hipError_t launch_heads(const QkNormArgs& a, hipStream_t st) {
   const int64_t lanes = (int64_t)a.n * (a.heads[0] + a.heads[1]) * LPH;
-  return lanes >= 4 * 8 * 64 * 1024 ? launch<T, LPH, 4>(a, st) : launch<T, LPH, 1>(a, st);
+  return lanes >= 4 * 2 * 64 * 1024 ? launch<T, LPH, 4>(a, st) : launch<T, LPH, 1>(a, st);
 }
 
 template <class T>

@@ -115,6 +115,16 @@ def test_norm_rope_options(kw, dtype, halves):
     run_norm(60, 6, 2, 64, dtype, 64, halves, seed=3, **kw)
 
 
+# So many rows that four heads share a row's factors.
+@pytest.mark.parametrize("kw", [dict(), dict(in_place=True, pad=5, extra=32)])
+@pytest.mark.parametrize("n,H,H_kv,d_h,dtype,d_rot,halves", [
+    (40000, 5, 2, 16, "bf16", 16, False), (30000, 3, 2, 32, "bf16", 32, True), (12000, 6, 1, 64, "bf16", 48, True),
+    (7000, 5, 3, 80, "bf16", 80, False), (4100, 9, 0, 128, "bf16", 128, True), (3001, 7, 2, 256, "bf16", 64, True),
+    (4000, 0, 9, 64, "f32", 64, False), (8200, 5, 3, 48, "f32", 16, True), (3000, 5, 1, 240, "f32", 240, True)])
+def test_norm_rope_many_rows(n, H, H_kv, d_h, dtype, d_rot, halves, kw):
+    run_norm(n, H, H_kv, d_h, dtype, d_rot, halves, seed=n + d_h, **kw)
+
+
 def test_norm_rope_padding_without_table():
     run_norm(40, 4, 4, 32, "bf16", 0, False, seed=4, pad=11)
 
