@@ -240,14 +240,15 @@ __device__ __noinline__ void careful_row(const T* q, const T* k, int64_t ks, con
 }
 
 // LDS of a work-group: the stage, and after the products for each wave 32 rows
-// of a segment of its partial rows (128 bytes, or the whole of a 64-byte row).
+// of a segment of its partial rows (128 bytes, or the whole of a 64-byte row); behind
+// them 2 KB per wave by which the queries come.
 template <class T, int D, int NT, int NW>
 struct TileLayout {
   static constexpr int CPR = D * (int)sizeof(T) / 16, ROWS = 32 * NT;
   static constexpr int VOFF = ROWS * CPR * 16, STAGE = 2 * VOFF;
   static constexpr int SEG = CPR < 8 ? CPR : 8;   // chunks of a segment
   static constexpr int OUT = NW * 32 * SEG * 16;
-  static constexpr int BYTES = STAGE > OUT ? STAGE : OUT;
+  static constexpr int QOFF = STAGE > OUT ? STAGE : OUT, BYTES = QOFF + NW * 2048;
   // chunk c of row r lies at chunk c ^ f(r): 16 rows at one chunk, or whole rows, per LDS cycle
   static __device__ __forceinline__ int f(int r) { return (r / (16 / SEG)) & (SEG - 1); }
 };
@@ -338,9 +339,34 @@ __global__ __launch_bounds__(64 * NW, D * sizeof(T) <= 256 ? (D * sizeof(T) <= 1
   float* ml = part.ML + 2 * (((oi * p.H_kv + hk) * p.slots + slot) * p.G + hg);
   const T* Qo = (const T*)p.Q + o * p.qo + (int64_t)i0 * p.qs + (int64_t)hk * p.G * D;
   const T* qp = Qo + qi * p.qs + hg * D;
+  // Q rows: four lanes read 64 bytes of one, a quarter of the cycles in the address
+  // unit that 32 rows side by side take (prompt 320 -> 312 us); the lanes' own chunks
+  // come by way of LDS, a segment of 32 rows x 64 bytes at a time (chunk c of row r at
+  // c ^ r / 4).
+  constexpr int NSEG = CPR / 4;
+  static_assert(NQ == 2 * NSEG, "two chunks of a segment per lane");
+  const int64_t qown = qi * p.qs + hg * D;
+  const int qr = lane >> 2, qx = ((lane & 3) ^ (qr >> 2)) & 3;
   u32x4 q[NQ];
 #pragma unroll
-  for (int k = 0; k < NQ; ++k) q[k] = gload((const u32x4*)(qp + (BF ? 16 * k + 8 * g : 8 * k + 4 * g)));
+  for (int h = 0; h < 2; ++h) {
+    const uint8_t* qs = (const uint8_t*)(Qo + __shfl(qown, qr + 16 * h, 64)) + 16 * qx;
+#pragma unroll
+    for (int s = 0; s < NSEG; ++s) q[2 * s + h] = gload((const u32x4*)(qs + 64 * s));
+  }
+  uint8_t* qb = lds + L::QOFF + wave * 2048;
+#pragma unroll
+  for (int s = 0; s < NSEG; ++s) {
+    *(u32x4*)(qb + lane * 16) = q[2 * s];
+    *(u32x4*)(qb + 1024 + lane * 16) = q[2 * s + 1];
+    __builtin_amdgcn_wave_barrier();
+    asm volatile("" ::: "memory");   // a wave's LDS accesses take place in order
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+      q[2 * s + j] = *(const u32x4*)(qb + l31 * 64 + (((2 * j + g) ^ (l31 >> 2)) & 3) * 16);
+    __builtin_amdgcn_wave_barrier();
+    asm volatile("" ::: "memory");
+  }
   f32x16 acc[NDT];
   if constexpr (!ONE) {
 #pragma unroll
