@@ -259,8 +259,9 @@ struct TileLayout {
 // transposed LDS reads); a row of the partial is one lane pair.  In bf16 the weights
 // are rounded for the products and summed as rounded, and partials are f16 times a
 // power of two of the row's own: 2^-11 of their largest values at most, an eighth of
-// what O's rounding to bf16 takes.  They are stored past the caches (4096 queries, 32
-// blocks each, with the merge's reads: 70 us, so 59).
+// what O's rounding to bf16 takes.  The merge reads them past the caches, where this
+// kernel leaves them (prompt: both plain 331 us, only stored past the caches 328, both
+// past them 312, so 308; grid 60, 62, 55, 55).
 template <class T, int D, int NT, int NW, bool ONE>
 __global__ __launch_bounds__(64 * NW, D * sizeof(T) <= 256 ? (D * sizeof(T) <= 128 || ONE ? 4 : 3) : 1) void k_block_tile(
     BlockAttendArgs p, BlockTileArgs w, BlockPartArgs part) {
@@ -547,7 +548,7 @@ __global__ __launch_bounds__(64 * NW, D * sizeof(T) <= 256 ? (D * sizeof(T) <= 1
     }
 #pragma unroll
     for (int k = 0; k < RN; ++k)
-      if ((rows_ok >> (rr0 + k * RPS)) & 1u) pstore((u32x4*)(ob + oo[k] + sg * L::SEG * 16), val[k]);
+      if ((rows_ok >> (rr0 + k * RPS)) & 1u) gstore((u32x4*)(ob + oo[k] + sg * L::SEG * 16), val[k]);
     __builtin_amdgcn_wave_barrier();
   }
 }
