@@ -67,10 +67,12 @@ struct AttendPlan {
 };
 
 // Partial rows of a chunk of queries, or of several objects': as much as the
-// memory-side cache holds until they are merged.  8192 queries, 16 heads of 128, 16
-// blocks each (537 MB, us): two chunks 2 x (108 + 51), one 230 + 148, three 3 x (87 +
-// 31).
-constexpr size_t PART_BYTES = (size_t)256 << 20;
+// memory-side cache holds until they are merged, but every chunk reads the keys and
+// values anew, so for a long cache up to twice its bytes.  537 MB of partials in chunks
+// of at most 160, 256 and 540 MB (us): 8192 queries of 512 blocks, 67 MB of keys
+// and values 341/318/325; of 2048 blocks, 268 MB 475/367/331; 4096 queries of 8192
+// blocks, 2.1 GB 1840/1188/747.
+constexpr size_t PART_LEAST = (size_t)256 << 20, PART_MOST = (size_t)1 << 30;
 
 void attend_plan(const rs3_block_shape* s, AttendPlan* a) {
   memset(a, 0, sizeof(*a));
@@ -100,11 +102,12 @@ void attend_plan(const rs3_block_shape* s, AttendPlan* a) {
   a->tile = s->n_q >= 8 && row_reads > tile_reads && n_blk <= BLOCK_TILE_MAX && n_blk > 0 && per_q <= (16u << 20) &&
             G <= 32 * BLOCK_TILE_WAVES;
   if (a->tile) {
-    // as many whole objects as PART_BYTES hold, or one and a chunk of its queries
-    const int64_t most_o = std::max<int64_t>(1, (int64_t)(PART_BYTES / (per_q * s->n_q)));
+    // as many whole objects as `part` holds, or one and a chunk of its queries
+    const size_t part = std::min(PART_MOST, std::max(PART_LEAST, (size_t)(2 * s->H_kv * s->n_kv * key_bytes)));
+    const int64_t most_o = std::max<int64_t>(1, (int64_t)(part / (per_q * s->n_q)));
     const int parts = (int)((s->n_obj + most_o - 1) / most_o);
     a->objs = (s->n_obj + parts - 1) / parts;
-    const int64_t most_q = std::max<int64_t>(64, (int64_t)(PART_BYTES / (per_q * a->objs)));
+    const int64_t most_q = std::max<int64_t>(64, (int64_t)(part / (per_q * a->objs)));
     a->chunks = (int)((s->n_q + most_q - 1) / most_q);
     a->chunk = (s->n_q + a->chunks - 1) / a->chunks;
     a->groups = a->objs * s->H_kv;
