@@ -127,7 +127,9 @@ __device__ void pick_row(const double* sc, const RowRange& r, int top_k, int32_t
   uint64_t kept[VPL];
 #pragma unroll
   for (int j = 0; j < VPL; ++j) kept[j] = j < seg ? key_at(j) : 0ull;
-  // scores at or above t[0..2], over the work-group: 21 bits of a counter each
+  // scores at or above t[0..2], over the work-group: 21 bits of a counter each, so
+  // that a wave's share of 2^21 blocks is counted one short (they are compared with
+  // at most 256)
   int slot = 0;
   if (tid < 3) sh.n[tid] = 0;
   for (int x = tid; x < BINS; x += 64 * NW) sh.bin[x] = 0;
@@ -143,6 +145,8 @@ __device__ void pick_row(const double* sc, const RowRange& r, int top_k, int32_t
 #pragma unroll
       for (int x = 0; x < 3; ++x) n[x] += (int)__popcll(__ballot(k >= t[x]));
     }
+#pragma unroll
+    for (int x = 0; x < 3; ++x) n[x] = min(n[x], (1 << 21) / NW - 1);
     if (lane == 0)
       atomicAdd(&sh.n[slot], (unsigned long long)n[0] | (unsigned long long)n[1] << 21 | (unsigned long long)n[2] << 42);
     __syncthreads();

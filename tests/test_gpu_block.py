@@ -279,6 +279,26 @@ def test_block_select_hard_scores_of_many_queries(make):
     run_select(3, 150, 15000, 4, 2, 64, 32, 11, 1, 1, "ragged", "bf16", seed=5, make=make)
 
 
+def test_block_select_most_blocks():
+    """2^21 blocks of one score, and of ascending ones."""
+    p = rs3()
+    n_blk, top_k = 1 << 21, 200
+    s = p.block_shape(p.RS3_BF16, 1, 1, n_blk * 32, 1, 1, 32, 32, top_k)
+    idx = torch.full((1, 1, 1, top_k), 77, dtype=torch.int32, device="cuda")
+    count = torch.full((1, 1, 1), 77, dtype=torch.int32, device="cuda")
+    Q = torch.ones((1, 1, 1, 32), dtype=torch.bfloat16, device="cuda")
+    M = torch.zeros((1, 1, n_blk, 32), dtype=torch.bfloat16, device="cuda")
+    ws = torch.empty(p.block_select_workspace_size(s), dtype=torch.uint8, device="cuda")
+    b = torch.arange(n_blk, device="cuda")
+    for first in (0, n_blk - top_k):
+        if first:   # scores b / 2^21, exact as three terms of seven bits
+            for c in range(3):
+                M[0, 0, :, c] = ((b >> (14 - 7 * c) & 127).float() * 2.0 ** (-7 * (c + 1))).bfloat16()
+        p.block_select(s, Q, M, idx, count, ws=ws)
+        torch.cuda.synchronize()
+        assert count.item() == top_k and torch.equal(idx.view(-1).cpu(), torch.arange(first, first + top_k, dtype=torch.int32))
+
+
 def test_block_select_nothing_to_read():
     p = rs3()
     s = p.block_shape(p.RS3_BF16, 2, 3, 0, 4, 2, 64, 32, 4)
