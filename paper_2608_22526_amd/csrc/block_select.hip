@@ -717,7 +717,18 @@ __global__ __launch_bounds__(64 * NWS, 4) void k_select_tile(BlockSelectArgs p, 
         for (int j = NV; j < seg; ++j) top = __builtin_elementwise_maximum(top, val_at(j));
         const float low = wave_min(top);   // 64 scores reach it, if each lane has one
         float vhi = wave_max(top) + eps2, vlo = rr.want <= 64 && low > -INFINITY ? low : -1.02f * qn[r] * sqrtf(k2) - eps2;
-        // few are wanted: first a value that at most 48 scores reach, and then on with
+        // few are wanted: a value that the largest of at most 32 lanes reach (about 44
+        // scores, if they lie anyhow), and then on with the scores from there, one per lane
+        if (rr.want <= 32 && low > -INFINITY) {
+          const float one[1] = {top};
+          float a = vlo, b = vhi;
+          narrow(one, 1, [](int) { return -INFINITY; }, rr.want, 32, eps2, a, b);
+          if (compact_row(kept, seg, val_at, a - eps2)) {
+            done_row(a, vhi);
+            continue;
+          }
+        }
+        // else first a value that at most 48 scores reach, and then on with
         // those alone, one per lane
         if (rr.want <= 48 && narrow(kept, seg, val_at, rr.want, 48, eps2, vlo, vhi) &&
             compact_row(kept, seg, val_at, vlo - eps2)) {
