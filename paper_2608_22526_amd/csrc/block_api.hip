@@ -174,7 +174,7 @@ void select_plan(const rs3_block_shape* s, BlockSelectPlan* a, size_t* ws) {
   if (s->n_q >= 4 && (rows > 256 || (s->n_q >= 8 && n_blk <= 256))) {
     int TR = 32;
     const int64_t heads = (int64_t)s->n_obj * s->H_kv;
-    while (TR > 4 && (before + TR * a->pitch * 4 > 81920 - 6144 || TR / 2 >= s->n_q || heads * ((s->n_q + TR - 1) / TR) < 256))
+    while (TR > 4 && (before + TR * a->pitch * 4 > 81920 - 10752 || TR / 2 >= s->n_q || heads * ((s->n_q + TR - 1) / TR) < 256))
       TR /= 2;
     int64_t lds = before + (int64_t)TR * a->pitch * 4;
     lds = std::max<int64_t>(lds, std::max<int64_t>(n_blk * 8, q_lds));

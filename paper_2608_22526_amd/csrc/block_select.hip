@@ -475,7 +475,7 @@ __global__ __launch_bounds__(64 * NWS, 4) void k_select_tile(BlockSelectArgs p, 
   __shared__ float qn[32], kn[NWS];
   __shared__ PickLds<NWS> sh;
   __shared__ int hard[32], n_hard, seen[32];
-  __shared__ u32x2 few[NWS][64];
+  __shared__ u32x4 room[NWS][64];   // of each wave: mean keys on their way, later a row's few scores
   const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5, l31 = lane & 31;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int64_t bid = folded_block(), og = bid / n_tile;
@@ -548,6 +548,13 @@ __global__ __launch_bounds__(64 * NWS, 4) void k_select_tile(BlockSelectArgs p, 
   float k2 = 0.f;   // the largest squared norm of a mean key
   for (int bt = wave; bt * 32 < nbm; bt += NWS) {
     const T* kp = km + (int64_t)min(bt * 32 + l31, nbm - 1) * D + 8 * half;
+    // bf16: four lanes read 64 bytes of a row (a quarter of the cycles in the address
+    // unit), 16 rows at a time go through LDS to the lanes of their chunks
+    const T* kq[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+      kq[h] = km + (int64_t)min(bt * 32 + 16 * h + (lane >> 2), nbm - 1) * D + 8 * (((lane & 3) ^ (lane >> 4)) & 3);
+    u32x4* mine = room[wave];
     f32x16 acc;
     float kk = 0.f;
     constexpr int KB = BF ? (NQ < 8 ? NQ : 8) : (NQ < 4 ? NQ : 4);
@@ -555,9 +562,34 @@ __global__ __launch_bounds__(64 * NWS, 4) void k_select_tile(BlockSelectArgs p, 
     for (int k0 = 0; k0 < NQ; k0 += KB) {
       u32x4 a[KB][BF ? 1 : 2];
 #pragma unroll
-      for (int k = 0; k < KB; ++k)
+      for (int k = 0; k < KB; ++k) {
+        if constexpr (BF) {
+          a[k][0] = gload((const u32x4*)(kq[k & 1] + 16 * (k0 + (k & ~1))));
+        } else {
 #pragma unroll
-        for (int y = 0; y < (BF ? 1 : 2); ++y) a[k][y] = gload((const u32x4*)(kp + 16 * (k0 + k)) + y);
+          for (int y = 0; y < 2; ++y) a[k][y] = gload((const u32x4*)(kp + 16 * (k0 + k)) + y);
+        }
+      }
+      if constexpr (BF) {
+#pragma unroll
+        for (int k = 0; k < KB; k += 2) {
+          u32x4 to[2];
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            mine[lane] = a[k + h][0];
+            __builtin_amdgcn_wave_barrier();
+            asm volatile("" ::: "memory");   // a wave's LDS accesses take place in order
+            if ((l31 >> 4) == h) {
+#pragma unroll
+              for (int j = 0; j < 2; ++j) to[j] = mine[(l31 & 15) * 4 + (((2 * j + half) ^ (l31 >> 2)) & 3)];
+            }
+            __builtin_amdgcn_wave_barrier();
+            asm volatile("" ::: "memory");
+          }
+          a[k][0] = to[0];
+          a[k + 1][0] = to[1];
+        }
+      }
 #pragma unroll
       for (int k = 0; k < KB; ++k) {
         u32x4 ah, al = {0, 0, 0, 0};
@@ -642,13 +674,14 @@ __global__ __launch_bounds__(64 * NWS, 4) void k_select_tile(BlockSelectArgs p, 
     // there are more than 64.
     float x = -INFINITY;
     int xb = 0;
+    u32x2* few = (u32x2*)room[wave];
     auto compact_row = [&](const float (&v)[NV], int n_seg, auto more, float t) {
       int n = 0;
       auto put = [&](int j, float y) {
         const uint64_t m = __ballot(y >= t);
         if (m == 0) return;
         const int at = n + (int)__popcll(m & below);
-        if (y >= t && at < 64) few[wave][at] = u32x2{__float_as_uint(y), (uint32_t)(64 * j + lane)};
+        if (y >= t && at < 64) few[at] = u32x2{__float_as_uint(y), (uint32_t)(64 * j + lane)};
         n += (int)__popcll(m);
       };
 #pragma unroll
@@ -658,7 +691,7 @@ __global__ __launch_bounds__(64 * NWS, 4) void k_select_tile(BlockSelectArgs p, 
       if (n > 64) return false;
       __builtin_amdgcn_s_waitcnt(0xc07f);   // lgkmcnt(0): written and read by this wave alone
       __builtin_amdgcn_wave_barrier();
-      const u32x2 y = few[wave][lane];
+      const u32x2 y = few[lane];
       __builtin_amdgcn_wave_barrier();
       x = lane < n ? __uint_as_float(y[0]) : -INFINITY;
       xb = (int)y[1];
