@@ -89,11 +89,11 @@ void attend_plan(const rs3_block_shape* s, AttendPlan* a) {
   // time as 128 KiB more for the row itself. The tile form reads each once, but has
   // five launches and the partial rows. Against 320 MiB and twice the cache (row and
   // tile form in us, 64-key blocks, bf16):
-  //   1 x n_q, 32/8 heads of 128, 16 of 256 blocks: n_q 32 16/31, 64 28/33, 128 52/37, 256 99/43
-  //   8 x n_q, the same of 128 blocks: n_q 8 34/49, 16 53/61, 32 95/74, 64 182/87
-  //   1 x n_q, 8/2 heads, 16 of 4096 blocks: n_q 256 42/62, 512 77/75, 1024 145/86
-  //   64 x n_q, 8/8 heads of 128, all 4 blocks: n_q 8 86/31, 64 622/44
-  //   1 x n_q, 8/8 heads of 64, fp32, 16 of 128 blocks of 32: n_q 32 12/24, 64 22/25, 128 41/27
+  //   1 x n_q, 32/8 heads of 128, 16 of 256 blocks: n_q 32 16/31, 64 28/33, 128 52/37, 256 100/43
+  //   8 x n_q, the same of 128 blocks: n_q 8 34/50, 16 53/62, 32 96/75, 64 182/90
+  //   1 x n_q, 8/2 heads, 16 of 4096 blocks: n_q 256 42/63, 512 77/76, 1024 144/89
+  //   64 x n_q, 8/8 heads of 128, all 4 blocks: n_q 8 84/31, 64 626/43
+  //   1 x n_q, 8/8 heads of 64, fp32, 16 of 128 blocks of 32: n_q 32 12/25, 64 22/26, 128 42/28
   const int64_t rows = (int64_t)s->n_obj * s->n_q * s->H_kv * ((G + 15) / 16);
   const int64_t key_bytes = (int64_t)2 * s->d_h * elem(s->dt);
   const int64_t keys = std::min<int64_t>((int64_t)slots * s->block, s->n_kv);
@@ -164,11 +164,11 @@ void select_plan(const rs3_block_shape* s, BlockSelectPlan* a, size_t* ws) {
   const int64_t n_blk = n_blocks(s), rows = (int64_t)s->n_obj * s->n_q * s->H_kv;
   a->split = 1;
   // Several queries (us, row form and tile form at 16 of 256 blocks, 8 key heads of
-  // 128: 256 rows 10.4/10.7, 512 19/11, 1024 36/11, 4096 131/15). The row form has a
+  // 128: 256 rows 10.5/10.1, 512 19/10, 1024 35/11, 4096 133/13). The row form has a
   // work-group per row, so up to one per CU it is no slower, and at many blocks faster
-  // (256 rows of 4096 blocks 49/94). The tile: the largest whose scores leave room for
+  // (256 rows of 4096 blocks 46/86). The tile: the largest whose scores leave room for
   // two work-groups per CU, smaller while that gives fewer work-groups than CUs (64
-  // queries: tiles of 32 19.5, of 4 10.8), at least four queries.
+  // queries: tiles of 32 18, of 4 10.3), at least four queries.
   const int q_lds = select_query_lds(s->d_h), before = s->d_h > 128 ? q_lds : 0;   // before the scores
   a->pitch = (int)((n_blk + 31) / 32 * 32 + 4);
   if (s->n_q >= 4 && (rows > 256 || (s->n_q >= 8 && n_blk <= 256))) {

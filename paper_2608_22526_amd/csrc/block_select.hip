@@ -14,7 +14,7 @@
 //      within that distance of it are scored again in fp64 (a few rows in a
 //      hundred, two or three blocks each), and where there are many of them (equal
 //      keys, zero queries, values that are no numbers) the whole row is.  4096 prompt
-//      tokens, 4 key heads of 128 and up to 512 blocks in 32 us: scores 15, the rest
+//      tokens, 4 key heads of 128 and up to 512 blocks in 30 us: scores 14, the rest
 //      the choice, which is bound by instruction issue.
 #include "block.h"
 

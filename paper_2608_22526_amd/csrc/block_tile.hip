@@ -15,7 +15,7 @@
 // 4096 queries, two heads of 128, 32 of 448 blocks of 64 keys in 55 us: counters 4,
 // lists 5 + 6, tiles 30 (262144 rows, 0.29 PFLOP/s), merge 13.5 (67 MB, 5 TB/s); all
 // pairs of these queries and keys take the dense kernel 125.  8192 prompt tokens, 16
-// heads of 128 to 4 key heads, 16 of up to 512 blocks in 313: tiles 2 x 110, merge 2 x
+// heads of 128 to 4 key heads, 16 of up to 512 blocks in 305 to 313: tiles 2 x 110, merge 2 x
 // 45.  No one unit bounds the tiles: a row moves 256 bytes of Q, 256 of its partial and
 // its share of 256 of the keys and values (address unit busy 57 % of the time; without
 // the stores 24 and 80 us), vector instructions issue in 40 % of the cycles, products
