@@ -456,7 +456,8 @@ def qk_norm_rope(n: int, Q, H: int, K, H_kv: int, d_h: int, dtype: int, Qo, Ko, 
                  ko_stride: Optional[int] = None, stream=None):
     """RMS norm of each head of Q [n][H][d_h] and K [n][H_kv][d_h] (None with
     0 heads) and the rotation of its first d_rot channels by table[pos]."""
-    _check_i32(n, H, H_kv, d_h, d_rot)
+    if (n | H | H_kv | d_h | d_rot) >> 31:
+        _check_i32(n, H, H_kv, d_h, d_rot)
     torch, dev, st = _call()
     dt, f32 = torch.bfloat16 if dtype == RS3_BF16 else torch.float32, torch.float32
     wq, wk = H * d_h, H_kv * d_h
@@ -519,7 +520,8 @@ def _shape_dtype(torch, s: BlockShape):
 def block_means(shape: BlockShape, K, Kmean, kv_len=None, n_new: int = 0, stream=None):
     """Kmean [n_obj][H_kv][n_blk][d_h]: the mean key of every block of K, or
     (n_new > 0) of the blocks that hold each object's last n_new keys."""
-    _check_i32(n_new)
+    if n_new >> 31:
+        _check_i32(n_new)
     torch, dev, st = _call()
     s, dt = shape, _shape_dtype(torch, shape)
     k = _rows(torch, "K", K, _span(s.n_obj, s.k_obj_stride, s.n_kv, s.k_stride, s.H_kv * s.d_h), dt, dev)

@@ -174,7 +174,8 @@ void select_plan(const rs3_block_shape* s, BlockSelectPlan* a, size_t* ws) {
   if (s->n_q >= 4 && (rows > 256 || (s->n_q >= 8 && n_blk <= 256))) {
     int TR = 32;
     const int64_t heads = (int64_t)s->n_obj * s->H_kv;
-    while (TR > 4 && (before + TR * a->pitch * 4 > 81920 - 10752 || TR / 2 >= s->n_q || heads * ((s->n_q + TR - 1) / TR) < 256))
+    while (TR > 4 && (before + TR * a->pitch * 4 > 81920 - 10752 || TR / 2 >= s->n_q ||
+                      heads * ((s->n_q + TR - 1) / TR) < 256))
       TR /= 2;
     int64_t lds = before + (int64_t)TR * a->pitch * 4;
     lds = std::max<int64_t>(lds, std::max<int64_t>(n_blk * 8, q_lds));
@@ -205,7 +206,8 @@ rs3_status rs3_qk_norm_rope(int32_t n, const void* Q, int64_t q_stride, int32_t 
                             const int32_t* pos, void* Qo, int64_t qo_stride, void* Ko, int64_t ko_stride,
                             void* stream) {
   if (n < 0 || n > (1 << 24) || (dt != RS3_BF16 && dt != RS3_F32)) return RS3_E_INVALID;
-  if (H < 0 || H_kv < 0 || H > 1024 || H_kv > 1024 - H || (int64_t)n * (H + H_kv) > (1 << 27) || d_h < 16 || d_h > 256 || d_h % 16 != 0) return RS3_E_INVALID;
+  if (H < 0 || H_kv < 0 || H > 1024 || H_kv > 1024 - H || d_h < 16 || d_h > 256 || d_h % 16 != 0) return RS3_E_INVALID;
+  if ((int64_t)n * (H + H_kv) > (1 << 27)) return RS3_E_INVALID;   // fewer than 2^32 threads
   if (!(eps > 0.f) || !isfinite(eps)) return RS3_E_INVALID;
   if (d_rot < 0 || d_rot > d_h || d_rot % 16 != 0 || (d_rot > 0) != (table != nullptr)) return RS3_E_INVALID;
   if (pairing != RS3_PAIRS_ADJACENT && pairing != RS3_PAIRS_HALVES) return RS3_E_INVALID;
