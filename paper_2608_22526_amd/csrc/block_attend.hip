@@ -25,7 +25,8 @@ __device__ __forceinline__ float max4(float v) {
 // of 16 so that more waves (and their SIMDs) find room.
 template <class T, int D>
 struct RowLayout {
-  static constexpr int CPR = D * (int)sizeof(T) / 16, KP = CPR >= 32 && sizeof(T) == 4 ? 16 : 32, VOFF = KP * CPR * 16, STAGE = 2 * VOFF, WAVE = 2 * STAGE;
+  static constexpr int CPR = D * (int)sizeof(T) / 16, KP = CPR >= 32 && sizeof(T) == 4 ? 16 : 32;
+  static constexpr int VOFF = KP * CPR * 16, STAGE = 2 * VOFF, WAVE = 2 * STAGE;
   static constexpr int NW = 131072 / WAVE < 4 ? 131072 / WAVE : 4;
   static constexpr int XP = D + 4;   // floats of a head's sums
   static_assert(16 * XP * 4 + 16 * 8 <= WAVE, "the sums fit the stages");
