@@ -112,10 +112,12 @@ void attend_plan(const rs3_block_shape* s, AttendPlan* a) {
     a->chunk = (s->n_q + a->chunks - 1) / a->chunks;
     a->groups = a->objs * s->H_kv;
     // queries of a counting work-group: four entries a thread, fewer while that leaves CUs
-    // idle and the blocks' counters are no more than the entries (2000 queries of 16/1
-    // heads, 4 of 7 blocks: 42 us with four work-groups, 38 with 32)
-    const int64_t spread = std::max<int64_t>((int64_t)a->chunk * a->chunks * a->groups / 256, n_blk / slots);
-    a->run = (int)std::max<int64_t>(64, std::min<int64_t>(2048 / slots, spread));
+    // idle and the entries are at least four times the blocks' counters (2000 queries of
+    // 16/1 heads, 4 of 7 blocks: 42 us with four work-groups, 38 with 63; 300 queries of
+    // 32/8, 256 blocks each: 279 with 64 queries per work-group, 257 with 16)
+    const int64_t spread = std::max<int64_t>((int64_t)a->chunk * a->chunks * a->groups / 256, 4 * n_blk / slots);
+    const int least = std::max(std::max(128 / slots, 16), s->n_q >> 15);
+    a->run = (int)std::max<int64_t>(least, std::min<int64_t>(2048 / slots, spread));
     a->runs = (a->chunk + a->run - 1) / a->run;
     a->tq = 32 * BLOCK_TILE_WAVES / G;
     const int64_t entries = (int64_t)a->chunk * slots;
