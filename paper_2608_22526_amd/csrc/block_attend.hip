@@ -38,7 +38,7 @@ struct RowLayout {
 // piece ahead, so that no barrier stands between the pieces.  The G query heads
 // of the key head are the columns of 16x16 products: S^T = K Q^T, and the
 // weights feed O^T += V^T P^T from their registers.  Keys past the last that
-// the query sees read that one again with weight 0.  In bf16 the weights are rounded
+// the query sees read that one again; their weights and values are 0.  In bf16 the weights are rounded
 // for the products (2^-8 of a weight, as O's own rounding), and their sum is of the
 // rounded ones.  Bound by the read of the keys and values: one token of 32 streams,
 // 32 heads of 128 to 8, 2048 of up to 16384 keys each, 269 MB in 50 us (5.4 TB/s).
@@ -140,7 +140,12 @@ __global__ __launch_bounds__(64 * NW) void k_block_row(BlockAttendArgs p, BlockP
       wait_vmcnt<0>();
     }
     asm volatile("" ::: "memory");   // the stage is read after the wait
-    const uint8_t* st = mine + slot * L::STAGE;
+    uint8_t* st = mine + slot * L::STAGE;
+    if (left < KP) {   // values that the query does not see count as 0 (0 times an infinity is no number)
+      for (int c = max(left, 0) * CPR + lane; c < KP * CPR; c += 64) *(u32x4*)(st + L::VOFF + c * 16) = u32x4{0, 0, 0, 0};
+      __builtin_amdgcn_wave_barrier();
+      asm volatile("" ::: "memory");   // a wave's LDS accesses take place in order
+    }
     f32x4 sc[NKT];
 #pragma unroll
     for (int kt = 0; kt < NKT; ++kt) sc[kt] = f32x4{0.f, 0.f, 0.f, 0.f};

@@ -6,6 +6,7 @@ formula makes an infinity or no number has to be that."""
 import numpy as np
 import pytest
 
+import test_gpu_block
 from oracle import block as B
 from test_gpu_block import U, check_attend, dev, dt_of, host, huge, not_finite, rs3, run_attend, run_select
 from workloads import storage_to_f64, to_storage
@@ -23,3 +24,51 @@ def test_forced_blocks_alone_fill_the_list(make, n_obj, n_q, n_kv, top_k, first,
     """No block is chosen, whatever its score: the list is the forced ones and
     its count no more than top_k."""
     run_select(n_obj, n_q, n_kv, 4, 2, 64, 32, top_k, first, last, vis, "bf16", seed=n_q + top_k, make=make)
+
+
+# ---- attend --------------------------------------------------------------------
+def check_values(got, Q, K, V, idx, count, v, block, dtype):
+    """check_attend where the result is finite, else the same infinity or no number."""
+    with np.errstate(all="ignore"):
+        O = B.block_attend(Q, K, V, idx, count, v, block)[0]
+    assert np.array_equal(np.isnan(got), np.isnan(O))
+    inf = np.isinf(O)
+    assert np.array_equal(np.isinf(got), inf) and np.array_equal(np.sign(got[inf]), np.sign(O[inf]))
+    W = np.where(np.isfinite(V), V, 0.0)
+    check_attend(np.where(np.isfinite(O), got, B.block_attend(Q, K, W, idx, count, v, block)[0]), Q, K, W, idx, count, v,
+                 block, dtype)
+    return O
+
+
+def every_block(rng, n_obj, n_q, H_kv, nb, top_k, wrong):
+    idx = np.broadcast_to(np.arange(nb, dtype=np.int32), (n_obj, n_q, H_kv, nb))
+    return idx.copy(), np.full((n_obj, n_q, H_kv), nb, np.int32)
+
+
+def infinite_values(at):
+    def edit(rng, Q, K, V, v):
+        inf = np.array([0x7F80, 0xFF80], np.uint16) if V.dtype == np.uint16 else np.array([np.inf, -np.inf], np.float32)
+        V[:, at, :, 5], V[:, at, :, V.shape[-1] - 1] = inf[0], inf[1]
+        return Q, K, V
+    return edit
+
+
+# Queries, keys, heads, width, block: a query per work-group, and (many rows) a block per work-group.
+@pytest.mark.parametrize("n_obj,n_q,n_kv,H,H_kv,d_h,block,dtype", [
+    (1, 1, 81, 2, 1, 64, 64, "bf16"), (2, 3, 333, 6, 2, 32, 32, "bf16"), (1, 2, 2017, 4, 2, 128, 64, "bf16"),
+    (3, 1, 70, 5, 1, 256, 128, "bf16"), (1, 40, 129, 2, 2, 128, 256, "bf16"), (1, 1, 81, 2, 1, 64, 64, "f32"),
+    (2, 3, 119, 4, 2, 128, 64, "f32"), (1, 2, 1001, 4, 1, 256, 64, "f32"), (3, 5, 60, 2, 2, 32, 128, "f32"),
+    (30, 60, 90, 4, 4, 64, 64, "bf16"), (8, 150, 333, 8, 4, 128, 128, "bf16"), (30, 60, 90, 2, 2, 64, 32, "f32")])
+def test_infinite_last_value(monkeypatch, n_obj, n_q, n_kv, H, H_kv, d_h, block, dtype):
+    """The last key that a query sees, inside a block, has an infinite value: those
+    channels of the row are infinite, the others as ever."""
+    monkeypatch.setattr(test_gpu_block, "lists", every_block)
+    for vis, at in (("all", n_kv - 1), ("ragged", n_kv * 2 // 3 | 1)):
+        some = infinite_values(at)
+
+        def edit(rng, Q, K, V, v):
+            if v is not None:   # not seen, last, or with keys behind it
+                v[:] = at + np.arange(1, v.size + 1).reshape(v.shape) % 4
+            return some(rng, Q, K, V, v)
+        got, args = run_attend(n_obj, n_q, n_kv, H, H_kv, d_h, block, -(-n_kv // block), vis, dtype, seed=n_kv + d_h, edit=edit)
+        assert np.isinf(check_values(got, *args)[..., 5]).any()
