@@ -213,7 +213,6 @@ __device__ __noinline__ void careful_row(const T* q, const T* k, int64_t ks, con
       }
       const float w = __builtin_amdgcn_exp2f(s - sub);
       l += w;
-      if (w == 0.f) continue;
 #pragma unroll
       for (int e = 0; e < E; ++e) acc[e] += on ? w * to_f32<T>(v[j * vs + lane + 64 * e]) : 0.f;
     }

@@ -72,3 +72,23 @@ def test_infinite_last_value(monkeypatch, n_obj, n_q, n_kv, H, H_kv, d_h, block,
             return some(rng, Q, K, V, v)
         got, args = run_attend(n_obj, n_q, n_kv, H, H_kv, d_h, block, -(-n_kv // block), vis, dtype, seed=n_kv + d_h, edit=edit)
         assert np.isinf(check_values(got, *args)[..., 5]).any()
+
+
+@pytest.mark.parametrize("n_obj", [1, 30])
+@pytest.mark.parametrize("dtype,d_h,G", [("bf16", 64, 1), ("bf16", 128, 4), ("f32", 64, 2)])
+def test_infinite_value_under_a_weight_of_0(monkeypatch, n_obj, dtype, d_h, G):
+    """A key that a query sees at a logit of -inf has weight 0, and 0 times an
+    infinite value is no number, whether or not the query sees all of the block."""
+    monkeypatch.setattr(test_gpu_block, "lists", every_block)
+    n_q = 96
+
+    def edit(rng, Q, K, V, v):
+        q, k = storage_to_f64(Q, dtype), storage_to_f64(K, dtype)
+        q[..., 1], k[..., 1], k[:, 70, :, 1] = 8.0, 0.0, -3e38     # below the fp32 range
+        v[0, -1] = 128
+        infinite_values(70)(rng, Q, K, V, v)
+        return to_storage(q.astype(np.float32), dtype), to_storage(k.astype(np.float32), dtype), V
+    got, args = run_attend(n_obj, n_q, 128, G, 1, d_h, 64, 2, "causal", dtype, seed=d_h, edit=edit)
+    v = args[5]
+    check_values(got, *args)
+    assert np.isnan(got[v > 70][..., 5]).all() and np.isfinite(got[v <= 70]).all() and (v <= 70).any()
