@@ -58,38 +58,36 @@ __global__ __launch_bounds__(256) void k_qk_norm(QkNormArgs p) {
     for (int e = 0; e < EPL; ++e) gain[e] = 1.f;
   }
   if (ps < 0 || (p.d_rot && ps >= p.n_pos)) return;
-  // factors of the lane's channels: 1 and 0 where it turns none, so that all
-  // lanes run the same way.  Halves: channel e times cs[e] plus its partner times
-  // sn[e]; adjacent: pair e/2 has (cs[e/2], sn[e/2])
+  // factors of the lane's channels (lanes that turn none read some and leave
+  // their values as they are).  Halves: channel e times cs[e] plus its partner
+  // times sn[e]; adjacent: pair e/2 has (cs[e/2], sn[e/2])
   float cs[EPL], sn[EPL];
 #pragma unroll
-  for (int e = 0; e < EPL; ++e) {
-    cs[e] = 1.f;
-    sn[e] = 0.f;
-  }
+  for (int e = 0; e < EPL; ++e) cs[e] = sn[e] = 0.f;
   const int hl = p.d_rot / 2 / EPL;   // lanes of a half
+  const bool turn = c0 < p.d_rot;
   int other = threadIdx.x & 63;
   if (p.d_rot) {
-    const bool turn = c0 < p.d_rot, lo = c < hl;
+    const bool lo = c < hl;
     const float* tab = p.table + (int64_t)ps * p.d_rot + (!turn ? 0 : p.halves ? 2 * EPL * (lo ? c : c - hl) : c0);
     if (p.halves) {
       if (turn) other += lo ? hl : -hl;
 #pragma unroll
       for (int e = 0; e < EPL; e += 2) {
         const f32x4 w = gload((const f32x4*)(tab + 2 * e));
-        cs[e] = turn ? w[0] : 1.f;
-        cs[e + 1] = turn ? w[2] : 1.f;
-        sn[e] = turn ? (lo ? -w[1] : w[1]) : 0.f;
-        sn[e + 1] = turn ? (lo ? -w[3] : w[3]) : 0.f;
+        cs[e] = w[0];
+        cs[e + 1] = w[2];
+        sn[e] = lo ? -w[1] : w[1];
+        sn[e + 1] = lo ? -w[3] : w[3];
       }
     } else {
 #pragma unroll
       for (int e = 0; e < EPL; e += 4) {
         const f32x4 w = gload((const f32x4*)(tab + e));
-        cs[e / 2] = turn ? w[0] : 1.f;
-        sn[e / 2] = turn ? w[1] : 0.f;
-        cs[e / 2 + 1] = turn ? w[2] : 1.f;
-        sn[e / 2 + 1] = turn ? w[3] : 0.f;
+        cs[e / 2] = w[0];
+        sn[e / 2] = w[1];
+        cs[e / 2 + 1] = w[2];
+        sn[e / 2 + 1] = w[3];
       }
     }
   }
@@ -119,13 +117,13 @@ __global__ __launch_bounds__(256) void k_qk_norm(QkNormArgs p) {
           for (int e = 0; e < EPL; ++e) y[e] = __shfl(x[e], other, 64);
         }
 #pragma unroll
-        for (int e = 0; e < EPL; ++e) x[e] = __builtin_fmaf(x[e], cs[e], y[e] * sn[e]);
+        for (int e = 0; e < EPL; ++e) x[e] = turn ? __builtin_fmaf(x[e], cs[e], y[e] * sn[e]) : x[e];
       } else {
 #pragma unroll
         for (int e = 0; e < EPL; e += 2) {
           const float a = x[e], b = x[e + 1];
-          x[e] = a * cs[e / 2] - b * sn[e / 2];
-          x[e + 1] = a * sn[e / 2] + b * cs[e / 2];
+          x[e] = turn ? a * cs[e / 2] - b * sn[e / 2] : a;
+          x[e + 1] = turn ? a * sn[e / 2] + b * cs[e / 2] : b;
         }
       }
     }

@@ -92,3 +92,27 @@ def test_infinite_value_under_a_weight_of_0(monkeypatch, n_obj, dtype, d_h, G):
     v = args[5]
     check_values(got, *args)
     assert np.isnan(got[v > 70][..., 5]).all() and np.isfinite(got[v <= 70]).all() and (v <= 70).any()
+
+
+# ---- norm and rotation ---------------------------------------------------------
+@pytest.mark.parametrize("halves", [False, True])
+@pytest.mark.parametrize("n,heads,d_h,d_rot,dtype", [
+    (5, 3, 64, 32, "bf16"), (5, 3, 256, 128, "bf16"), (4100, 9, 256, 128, "bf16"), (5, 2, 80, 48, "f32"),
+    (5, 2, 128, 64, "f32"), (3000, 5, 240, 16, "f32"), (5, 3, 96, 0, "bf16")])
+def test_norm_rope_infinite_channel(halves, n, heads, d_h, d_rot, dtype):
+    """An infinite value makes its own channel, and the one that it is turned
+    with, no number (the row's root is infinite, and the others are 0)."""
+    p, rng = rs3(), np.random.default_rng(d_h)
+    x = to_storage(rng.standard_normal((n, heads, d_h), dtype=np.float32), dtype)
+    at = rng.integers(0, d_h, (n, heads))
+    inf = np.where(rng.random((n, heads)) < 0.5, np.inf, -np.inf).astype(np.float32)
+    np.put_along_axis(x, at[..., None], to_storage(inf, dtype)[..., None], -1)
+    table = rng.uniform(0.5, 1.0, (n, max(d_rot, 2) // 2, 2)).astype(np.float32)
+    X, Y = dev(x), torch.full(x.shape, 7.0, dtype=dev(x).dtype, device="cuda")
+    p.qk_norm_rope(n, X, heads, None, 0, d_h, dt_of(dtype), Y, None, eps=1e-5, table=dev(table) if d_rot else None,
+                   d_rot=d_rot, pairing=p.RS3_PAIRS_HALVES if halves else p.RS3_PAIRS_ADJACENT)
+    torch.cuda.synchronize()
+    with np.errstate(all="ignore"):
+        exp = B.norm_rope(storage_to_f64(x, dtype), None, 1e-5, table if d_rot else None, None, halves)
+    got = host(Y, dtype)
+    assert np.array_equal(np.isnan(got), np.isnan(exp)) and (got[~np.isnan(exp)] == 0).all()
