@@ -137,10 +137,18 @@ __device__ __forceinline__ float to_f32(T v) {
   if constexpr (sizeof(T) == 2) return bf2f(v);
   else return v;
 }
+
+// Rounded once: to bf16 by way of the fp32 number whose last bit says whether
+// anything is behind it (toward zero, set if so), which has bits to spare for that.
 template <class T>
-__device__ __forceinline__ T from_f32(float v) {
-  if constexpr (sizeof(T) == 2) return f2bf(v);
-  else return v;
+__device__ __forceinline__ T from_f64(double v) {
+  const float f = (float)v;
+  if constexpr (sizeof(T) == 4) return f;
+  else {
+    uint32_t u = __float_as_uint(f);
+    if ((double)f != v) u = (u - (__builtin_fabs((double)f) > __builtin_fabs(v))) | 1u;
+    return f2bf(__uint_as_float(u));
+  }
 }
 
 }  // namespace rs3

@@ -6,7 +6,7 @@ namespace rs3 {
 // grid (blocks, H_kv, n_obj), block 256: d_h/EPL lanes read a key row in
 // 16-byte chunks, the groups of lanes take the block's rows in turn, and the
 // groups' fp64 sums meet in LDS.  bf16 keys add up exactly in fp64 unless a
-// channel's values span more than 2^39, so that the rounded mean does not
+// channel's values span more than 2^45 / block, so that the rounded mean does not
 // depend on the order.  Bound by the read of the keys: 65536 keys of 8 heads of 128
 // in bf16, 136 MB in 26.8 us (5.1 TB/s); the newest blocks of 64 caches in 4 us, a
 // launch and a round trip.
@@ -45,7 +45,7 @@ __global__ __launch_bounds__(256) void k_block_means(BlockMeansArgs p) {
     double t = 0.0;
     for (int i = 0; i < groups; ++i) t += part[(d % EPL) * 256 + i * cpr + d / EPL];
     ((T*)p.Kmean)[(((int64_t)o * p.H_kv + h) * p.n_blk + b) * p.d_h + d] =
-        from_f32<T>(keys > 0 ? (float)(t / keys) : 0.f);
+        from_f64<T>(keys > 0 ? t / keys : 0.0);
   }
 }
 

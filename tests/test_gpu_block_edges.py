@@ -116,3 +116,50 @@ def test_norm_rope_infinite_channel(halves, n, heads, d_h, d_rot, dtype):
         exp = B.norm_rope(storage_to_f64(x, dtype), None, 1e-5, table if d_rot else None, None, halves)
     got = host(Y, dtype)
     assert np.array_equal(np.isnan(got), np.isnan(exp)) and (got[~np.isnan(exp)] == 0).all()
+
+
+# ---- means ---------------------------------------------------------------------
+def bf16_of(x):
+    """fp64 to the nearest bf16 in one rounding, ties to even (normal results)."""
+    m, e = np.frexp(x)
+    return np.ldexp(np.rint(np.ldexp(m, 8)), e - 8)
+
+
+def run_means(K, block, kv_len=None):
+    p = rs3()
+    n_obj, n_kv, H_kv, d_h = K.shape
+    M = torch.full((n_obj, H_kv, -(-n_kv // block), d_h), 9.0, device="cuda", dtype=torch.bfloat16)
+    p.block_means(p.block_shape(p.RS3_BF16, n_obj, 1, n_kv, H_kv, H_kv, d_h, block, 1), dev(K), M,
+                  kv_len=None if kv_len is None else dev(kv_len))
+    torch.cuda.synchronize()
+    return host(M, "bf16"), B.block_means(storage_to_f64(K, "bf16"), [n_kv] * n_obj if kv_len is None else kv_len, block)
+
+
+def test_means_are_rounded_once():
+    """Means a little beside the middle of two bf16 numbers, by less than fp32
+    tells apart, and on it; of either sign and of any size."""
+    rng = np.random.default_rng(1)
+    k = np.zeros((1, 4, 3, 64))
+    k[0, :2] = rng.choice([(2.0, 2.015625), (2.015625, 2.03125), (2.5, 2.515625)], (3, 64)).transpose(2, 0, 1)
+    k[0, 2] = rng.choice([-1, 0, 1], (3, 64)) * 2.0 ** -rng.integers(24, 40, (3, 64))
+    k *= rng.choice([-1, 1], (3, 64)) * 2.0 ** rng.integers(-60, 100, (3, 64))
+    got, exp = run_means(to_storage(k.astype(np.float32), "bf16"), 32)
+    assert (bf16_of(exp) != bf16_of(exp.astype(np.float32).astype(np.float64))).any()
+    assert np.array_equal(got, bf16_of(exp))
+
+
+@pytest.mark.parametrize("d_h,block", [(32, 32), (64, 64), (128, 128), (256, 256)])
+def test_means_of_ordinary_keys_are_the_nearest(d_h, block):
+    rng = np.random.default_rng(block)
+    K = to_storage(rng.standard_normal((3, 700, 2, d_h), dtype=np.float32), "bf16")
+    got, exp = run_means(K, block, np.array([700, 0, 333], np.int32))
+    assert np.array_equal(got, bf16_of(exp))
+
+
+def test_means_of_infinite_and_largest_keys():
+    big = storage_to_f64(np.array([0x7F7F], np.uint16), "bf16")[0]
+    k = np.zeros((1, 2, 1, 32))
+    k[0, :, 0, :6] = np.array([(np.inf, 1), (-np.inf, 1), (np.inf, -np.inf), (np.nan, 1), (big, big), (-big, -big)]).T
+    with np.errstate(invalid="ignore"):
+        got = run_means(to_storage(k.astype(np.float32), "bf16"), 32)[0][0, 0, 0]
+    assert np.array_equal(got[:6], [np.inf, -np.inf, np.nan, np.nan, big, -big], equal_nan=True) and (got[6:] == 0).all()
