@@ -599,9 +599,14 @@ rs3_status rs3_stack_readout(const rs3_stack* S, const rs3_grid* g, const void* 
  * enabled, each kernel launched by the library is bracketed by two events on
  * its stream (event records only: nothing is allocated or synchronised in the
  * timed calls; launches beyond the pool are not timed and are counted as
- * dropped).  rs3_profile_report waits for the recorded events and fills
- * total_ms[RS3_K_COUNT] and launches[RS3_K_COUNT] (host arrays) with the
- * accumulated kernel durations per kernel id; rs3_profile_reset clears them. */
+ * dropped).  rs3_profile_report_n waits for the recorded events and fills
+ * total_ms[n] and launches[n] (host arrays) with the accumulated kernel
+ * durations per kernel id (0 past the ids of this library); rs3_profile_reset
+ * clears them.  RS3_K_COUNT grows with new kernels, so a program passes the
+ * length it was built with: rs3_profile_report does, for arrays of
+ * RS3_K_COUNT.  The function of that name, which programs built on earlier
+ * headers call, fills the ids up to RS3_K_STACK_ROWS, all that there were when it
+ * took no length, and nothing past them. */
 enum {
   RS3_K_ENERGY = 0,        /* token energies */
   RS3_K_SELECT = 1,        /* prior + top-k + compaction */
@@ -624,7 +629,10 @@ enum {
   RS3_K_COUNT = 18
 };
 rs3_status rs3_profile_enable(int32_t on, int32_t max_launches);
+rs3_status rs3_profile_report_n(int32_t n, double* total_ms, int64_t* launches, int64_t* dropped);
 rs3_status rs3_profile_report(double* total_ms, int64_t* launches, int64_t* dropped);
+#define rs3_profile_report(total_ms, launches, dropped) \
+  rs3_profile_report_n(RS3_K_COUNT, (total_ms), (launches), (dropped))
 rs3_status rs3_profile_reset(void);
 
 /* ---- read-only streaming rate (measurement) --------------------------------

@@ -115,6 +115,7 @@ _SIGS = {
     "rs3_block_attend": (c_i32, [ctypes.POINTER(BlockShape), c_vp, c_vp, c_vp, c_vp, c_vp, c_vp, c_vp, c_vp, c_sz,
                                  c_vp]),
     "rs3_profile_enable": (c_i32, [c_i32, c_i32]),
+    "rs3_profile_report_n": (c_i32, [c_i32, c_vp, c_vp, c_vp]),
     "rs3_profile_report": (c_i32, [c_vp, c_vp, c_vp]),
     "rs3_profile_reset": (c_i32, []),
     "rs3_stream_read": (c_i32, [c_vp, c_sz, c_vp, c_vp]),
@@ -643,7 +644,7 @@ def profile_report() -> dict:
     ms = np.zeros(n, np.float64)
     cnt = np.zeros(n, np.int64)
     dropped = np.zeros(1, np.int64)
-    _check(lib().rs3_profile_report(ms.ctypes.data, cnt.ctypes.data, dropped.ctypes.data), "rs3_profile_report")
+    _check(lib().rs3_profile_report_n(n, ms.ctypes.data, cnt.ctypes.data, dropped.ctypes.data), "rs3_profile_report_n")
     out = {KERNEL_NAMES[i]: (float(ms[i]), int(cnt[i])) for i in range(n)}
     out["_dropped"] = (0.0, int(dropped[0]))
     return out

@@ -1,7 +1,7 @@
 // Optional per-kernel timing with HIP events.  When enabled, every kernel the
 // library launches carries a pair of events that the runtime stamps with the
 // kernel's own start and end (hipExtLaunchKernelGGL);
-// rs3_profile_report() waits for them and returns per-kernel totals.
+// rs3_profile_report_n() waits for them and returns per-kernel totals.
 // The event pool is created at enable time, so timed calls allocate nothing.
 #include <vector>
 
@@ -96,15 +96,20 @@ rs3_status rs3_profile_enable(int32_t on, int32_t max_launches) {
   return RS3_OK;
 }
 
-rs3_status rs3_profile_report(double* total_ms, int64_t* launches, int64_t* dropped) {
-  if (!total_ms || !launches) return RS3_E_INVALID;
+rs3_status rs3_profile_report_n(int32_t n, double* total_ms, int64_t* launches, int64_t* dropped) {
+  if (n < 0 || !total_ms || !launches) return RS3_E_INVALID;
   if (fold() != hipSuccess) return RS3_E_DEVICE;
-  for (int i = 0; i < RS3_K_COUNT; ++i) {
-    total_ms[i] = P.total_ms[i];
-    launches[i] = P.count[i];
+  for (int i = 0; i < n; ++i) {
+    total_ms[i] = i < RS3_K_COUNT ? P.total_ms[i] : 0.0;
+    launches[i] = i < RS3_K_COUNT ? P.count[i] : 0;
   }
   if (dropped) *dropped = P.dropped;
   return RS3_OK;
+}
+
+// (the function: in parentheses the header's macro does not apply)
+rs3_status (rs3_profile_report)(double* total_ms, int64_t* launches, int64_t* dropped) {
+  return rs3_profile_report_n(RS3_K_STACK_ROWS + 1, total_ms, launches, dropped);
 }
 
 rs3_status rs3_stream_read(const void* src, size_t bytes, uint32_t* out, void* stream) {
