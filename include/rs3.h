@@ -508,7 +508,11 @@ rs3_status rs3_block_means(const rs3_block_shape* s /*[host]*/, const void* K, c
  * the lower block.
  * idx   : out int32 [n_obj][n_q][H_kv][top_k], ascending, -1 past the count
  * count : out int32 [n_obj][n_q][H_kv]
- * ws    : at least rs3_block_select_workspace_size() bytes */
+ * ws    : at least rs3_block_select_workspace_size() bytes: scores, for few
+ *         queries and past 16,384 blocks, at most 256 MiB of them (more rows than
+ *         those of that many scores are taken in parts, one after the other)
+ * Many queries are scored together up to about 8,100 blocks (6,100 with heads
+ * of 256); past those every query reads all mean keys for itself. */
 rs3_status rs3_block_select_workspace_size(const rs3_block_shape* s /*[host]*/, size_t* bytes);
 rs3_status rs3_block_select(const rs3_block_shape* s /*[host]*/, const void* Q, const void* Kmean,
                             const int32_t* n_vis, int32_t* idx, int32_t* count, void* ws, size_t ws_bytes,

@@ -33,8 +33,8 @@ struct BlockSelectArgs {
   const int32_t* n_vis;    // [n_obj][n_q] or null
   int32_t* idx;            // [n_obj][n_q][H_kv][top_k]
   int32_t* count;          // [n_obj][n_q][H_kv]
-  double* score;           // [rows][n_blk] workspace, or null
-  int64_t rows;            // n_obj * n_q * H_kv
+  double* score;           // [end - row0][n_blk] workspace, or null
+  int64_t row0, end;       // rows of this launch, of the n_obj * n_q * H_kv (row forms)
   int n_obj, n_q, n_kv, H, H_kv, d_h, block, n_blk, top_k, n_first, n_last;
 };
 
@@ -46,6 +46,7 @@ struct BlockSelectPlan {
   bool tile;         // several queries of a key head per work-group, else one
   int TR, pitch;     // tile: queries, floats of a row of scores
   int split;         // else: work-groups that share a row's blocks, whose scores go to the workspace (1: LDS)
+  int64_t at_once;   //   and the rows that are there at a time
   int lds;
 };
 

@@ -163,6 +163,10 @@ rs3_status ensure_setup() {
   return RS3_OK;
 }
 
+// Scores in the workspace of the block choice: the rows beyond take it again (16
+// rows of 2^21 blocks, the most that there can be, and what the memory-side cache holds).
+constexpr size_t SCORES_MOST = (size_t)256 << 20;
+
 void select_plan(const rs3_block_shape* s, BlockSelectPlan* a, size_t* ws) {
   memset(a, 0, sizeof(*a));
   *ws = 0;
@@ -197,8 +201,14 @@ void select_plan(const rs3_block_shape* s, BlockSelectPlan* a, size_t* ws) {
   int64_t split = rows > 0 && rows < 128 ? std::min<int64_t>(256 / rows, n_blk / 128) : 1;
   if (n_blk * 8 > SELECT_LDS) split = std::max<int64_t>(split, (n_blk + 4095) / 4096);
   a->split = (int)(split < 1 ? 1 : split);
-  if (a->split > 1) *ws = (size_t)rows * n_blk * sizeof(double);
-  else a->lds = (int)std::max<int64_t>(n_blk * 8, 16);
+  if (a->split > 1) {   // rows in parts of about one size
+    const int64_t most = (int64_t)(SCORES_MOST / (n_blk * sizeof(double)));
+    const int64_t parts = std::max<int64_t>(1, (rows + most - 1) / most);
+    a->at_once = (rows + parts - 1) / parts;
+    *ws = (size_t)a->at_once * n_blk * sizeof(double);
+  } else {
+    a->lds = (int)std::max<int64_t>(n_blk * 8, 16);
+  }
 }
 
 }  // namespace
@@ -305,7 +315,6 @@ rs3_status rs3_block_select(const rs3_block_shape* s, const void* Q, const void*
   a.idx = idx;
   a.count = count;
   a.score = (double*)ws;
-  a.rows = (int64_t)s->n_obj * s->n_q * s->H_kv;
   a.n_obj = s->n_obj;
   a.n_q = s->n_q;
   a.n_kv = s->n_kv;

@@ -391,12 +391,12 @@ template <class T, int D, bool SPLIT>
 __global__ __launch_bounds__(64 * NWR) void k_select_row(BlockSelectArgs p, int per) {
   extern __shared__ double sc[];
   __shared__ PickLds<NWR> sh;
-  const int64_t row = folded_block(), oi = row / p.H_kv;
-  if (row >= p.rows) return;
+  const int64_t row = p.row0 + folded_block(), oi = row / p.H_kv;
+  if (row >= p.end) return;
   const int g = (int)(row - oi * p.H_kv);
   const RowRange r = row_range(p, oi);
   const int a = max(SPLIT ? (int)blockIdx.z * per : 0, r.f_lo), b = min(SPLIT ? (int)(blockIdx.z + 1) * per : r.nb, r.last0);
-  double* out = SPLIT ? p.score + row * p.n_blk : sc;
+  double* out = SPLIT ? p.score + (row - p.row0) * p.n_blk : sc;
   if (r.want > 0 && a < b) score_row<T, D, NWR>(p, query_of<T>(p, oi, g, D), means_of<T>(p, oi, g, D), a, b, out);
   if constexpr (!SPLIT) {
     __syncthreads();
@@ -407,9 +407,9 @@ __global__ __launch_bounds__(64 * NWR) void k_select_row(BlockSelectArgs p, int 
 // The lists from scores in the workspace.
 __global__ __launch_bounds__(64 * NWR) void k_select_pick(BlockSelectArgs p) {
   __shared__ PickLds<NWR> sh;
-  const int64_t row = folded_block();
-  if (row >= p.rows) return;
-  pick_row<NWR>(p.score + row * p.n_blk, row_range(p, row / p.H_kv), p.top_k, p.idx + row * p.top_k, p.count + row, sh);
+  const int64_t row = p.row0 + folded_block();
+  if (row >= p.end) return;
+  pick_row<NWR>(p.score + (row - p.row0) * p.n_blk, row_range(p, row / p.H_kv), p.top_k, p.idx + row * p.top_k, p.count + row, sh);
 }
 
 __device__ __forceinline__ int pop(bool x) { return (int)__popcll(__ballot(x)); }
@@ -874,19 +874,27 @@ __global__ __launch_bounds__(64 * NWS, 4) void k_select_tile(BlockSelectArgs p, 
 }
 
 template <class T, int D>
-hipError_t launch(const BlockSelectArgs& a, const BlockSelectPlan& pl, hipStream_t st) {
+hipError_t launch(BlockSelectArgs a, const BlockSelectPlan& pl, hipStream_t st) {
+  const int64_t rows = (int64_t)a.n_obj * a.n_q * a.H_kv;
+  a.row0 = 0;
+  a.end = rows;
   if (pl.tile) {
     const int n_tile = (a.n_q + pl.TR - 1) / pl.TR;
     const int64_t n = (int64_t)a.n_obj * a.H_kv * n_tile;
     RS3_LAUNCH(RS3_K_BLOCK_SELECT, st, (k_select_tile<T, D>), folded(n), dim3(64 * NWS), pl.lds, st, a, pl.TR,
                n_tile, pl.pitch);
   } else if (pl.split > 1) {
-    RS3_LAUNCH(RS3_K_BLOCK_SELECT, st, (k_select_row<T, D, true>), folded(a.rows, pl.split), dim3(64 * NWR), 0, st,
-               a, (a.n_blk + pl.split - 1) / pl.split);
-    RS3_LAUNCH(RS3_K_BLOCK_SELECT, st, k_select_pick, folded(a.rows), dim3(64 * NWR), 0, st, a);
+    for (; a.row0 < rows; a.row0 += pl.at_once) {
+      const int64_t n = std::min(pl.at_once, rows - a.row0);
+      a.end = a.row0 + n;
+      RS3_LAUNCH(RS3_K_BLOCK_SELECT, st, (k_select_row<T, D, true>), folded(n, pl.split), dim3(64 * NWR), 0, st, a,
+                 (a.n_blk + pl.split - 1) / pl.split);
+      RS3_LAUNCH(RS3_K_BLOCK_SELECT, st, k_select_pick, folded(n), dim3(64 * NWR), 0, st, a);
+      const hipError_t e = hipGetLastError();
+      if (e != hipSuccess) return e;
+    }
   } else {
-    RS3_LAUNCH(RS3_K_BLOCK_SELECT, st, (k_select_row<T, D, false>), folded(a.rows), dim3(64 * NWR), pl.lds, st, a,
-               a.n_blk);
+    RS3_LAUNCH(RS3_K_BLOCK_SELECT, st, (k_select_row<T, D, false>), folded(rows), dim3(64 * NWR), pl.lds, st, a, a.n_blk);
   }
   return hipGetLastError();
 }

@@ -53,3 +53,19 @@ def test_timing_report_of_a_program_built_on_the_header(p, tmp_path):
     subprocess.check_call([cc, "-I", os.path.join(ROOT, "include"), str(src), "-o", str(exe), os.path.join(lib, "librs3.so"),
                            "-Wl,-rpath," + lib, "-Wl,-rpath,/opt/rocm/lib", "-Wl,--allow-shlib-undefined"])
     assert subprocess.check_output([str(exe)]) == b"0 0 -7"
+
+
+def select_bytes(p, n_q, n_kv, H, H_kv, d_h, block, top_k, n_obj=1, dt=1):
+    return p.block_select_workspace_size(p.block_shape(p.RS3_BF16 if dt else p.RS3_F32, n_obj, n_q, n_kv, H, H_kv, d_h, block,
+                                                       top_k))
+
+
+def test_select_workspace_does_not_grow_with_the_queries(p):
+    """At most 256 MiB of scores, at any size that is accepted."""
+    for case in ((4096, 524289, 32, 8, 128, 32, 16), (32768, 1100000, 32, 8, 128, 64, 16), (1 << 22, 1 << 26, 256, 256, 32, 32, 256),
+                 (32768, 1 << 22, 8, 8, 128, 64, 16), (1, 1 << 26, 256, 256, 32, 32, 256), (1, 1 << 20, 8, 8, 64, 64, 8, 4096),
+                 (100, 1 << 24, 4, 2, 64, 32, 9, 77, 0)):
+        assert select_bytes(p, *case) <= 256 << 20, case
+    assert select_bytes(p, 0, 1 << 26, 8, 8, 128, 32, 16) == 0
+    # as long as they fit, the scores of all rows
+    assert select_bytes(p, 1, 1 << 20, 8, 8, 128, 64, 16) == 8 * (1 << 14) * 8

@@ -163,3 +163,38 @@ def test_means_of_infinite_and_largest_keys():
     with np.errstate(invalid="ignore"):
         got = run_means(to_storage(k.astype(np.float32), "bf16"), 32)[0][0, 0, 0]
     assert np.array_equal(got[:6], [np.inf, -np.inf, np.nan, np.nan, big, -big], equal_nan=True) and (got[6:] == 0).all()
+
+
+# ---- calls that are taken in parts ------------------------------------------------
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_block_select_of_more_rows_than_the_scores_workspace_holds(dtype):
+    """2,406 rows of 16,385 blocks: the same lists as object by object, and at the
+    parts' border those of the oracle."""
+    p, rng = rs3(), np.random.default_rng(3)
+    n_obj, n_q, H, H_kv, d_h, block, top_k, n_kv = 3, 401, 4, 2, 32, 32, 11, 524289
+    nb = -(-n_kv // block)
+    Q = to_storage(rng.standard_normal((n_obj, n_q, H, d_h), dtype=np.float32), dtype)
+    M = to_storage(rng.standard_normal((n_obj, H_kv, nb, d_h), dtype=np.float32), dtype)
+    v = rng.integers(0, n_kv + 1, (n_obj, n_q)).astype(np.int32)
+    v[:, ::7] = n_kv
+
+    def run(o):
+        n = Q[o].shape[0]
+        s = p.block_shape(dt_of(dtype), n, n_q, n_kv, H, H_kv, d_h, block, top_k, 1, 2)
+        idx = torch.full((n, n_q, H_kv, top_k), 77, dtype=torch.int32, device="cuda")
+        count = torch.full((n, n_q, H_kv), 77, dtype=torch.int32, device="cuda")
+        ws = torch.full((p.block_select_workspace_size(s),), 0xFF, dtype=torch.uint8, device="cuda")
+        p.block_select(s, dev(Q[o]), dev(M[o]), idx, count, n_vis=dev(v[o]), ws=ws)
+        torch.cuda.synchronize()
+        return idx.cpu().numpy(), count.cpu().numpy(), ws.numel()
+    idx, count, size = run(slice(0, n_obj))
+    assert size < n_obj * n_q * H_kv * nb * 8      # more than one part
+    for o in range(n_obj):
+        i1, c1, _ = run(slice(o, o + 1))
+        assert np.array_equal(idx[o:o + 1], i1) and np.array_equal(count[o:o + 1], c1)
+    border = size // (nb * 8) // H_kv
+    for at in (0, border - 1, border, border + 1, n_obj * n_q - 1):
+        o, i = divmod(at, n_q)
+        ei, ec = B.block_select(storage_to_f64(Q[o:o + 1, i:i + 1], dtype), storage_to_f64(M[o:o + 1], dtype),
+                                v[o:o + 1, i:i + 1], block, top_k, 1, 2, n_kv)
+        assert np.array_equal(idx[o, i], ei[0, 0]) and np.array_equal(count[o, i], ec[0, 0])
