@@ -525,8 +525,10 @@ rs3_status rs3_block_select(const rs3_block_shape* s /*[host]*/, const void* Q, 
  * takes no part.
  * Logits of -inf have weight 0.  The bf16 form rounds the weights to bf16 for
  * the matrix cores; sums are fp32, and O is rounded to `dt` once.
- * ws : at least rs3_block_attend_workspace_size() bytes (for many queries lists
- *      and up to 1 GiB of partial rows, those of a chunk of the queries at a time) */
+ * ws : at least rs3_block_attend_workspace_size() bytes: for many queries up to
+ *      1 GiB of partial rows, those of a chunk of the queries at a time, and 256 MiB
+ *      of lists and (m, l) pairs, or those of one chunk (an eighth of K and V and
+ *      less than a third of the partial rows); few queries need little or none */
 rs3_status rs3_block_attend_workspace_size(const rs3_block_shape* s /*[host]*/, size_t* bytes);
 rs3_status rs3_block_attend(const rs3_block_shape* s /*[host]*/, const void* Q, const void* K, const void* V,
                             const int32_t* idx, const int32_t* count, const int32_t* n_vis, void* O, void* ws,

@@ -62,7 +62,8 @@ struct AttendPlan {
   bool tile;         // tiled form
   int S;             // splits of a row's keys (other form)
   int objs;          // objects at a time
-  int groups, chunk, chunks, run, runs, tq, tcap;
+  int groups, chunk, chunks, run, runs, tq, tcap;   // chunks: of a section
+  int64_t section;   // queries of an object whose lists are there at a time, whole chunks
   size_t ord, cnt, base, list, tiles, opart, ml, total;
 };
 
@@ -73,6 +74,9 @@ struct AttendPlan {
 // and values 341/318/325; of 2048 blocks, 268 MB 475/367/331; 4096 queries of 8192
 // blocks, 2.1 GB 1840/1188/747.
 constexpr size_t PART_LEAST = (size_t)256 << 20, PART_MOST = (size_t)1 << 30;
+// Lists and (m, l) pairs of a section of the queries (chunks, one at least): their
+// three launches take about 15 us, a chunk's own several times that.
+constexpr size_t LISTS_MOST = (size_t)256 << 20;
 
 void attend_plan(const rs3_block_shape* s, AttendPlan* a) {
   memset(a, 0, sizeof(*a));
@@ -128,13 +132,20 @@ void attend_plan(const rs3_block_shape* s, AttendPlan* a) {
   }
   if (a->tile) {
     const int64_t entries = (int64_t)a->chunk * slots;
-    a->ord = take((size_t)s->n_q * slots * a->groups * 4);
-    a->cnt = take((size_t)a->chunks * a->groups * n_blk * 4);
-    a->base = take((size_t)a->chunks * a->runs * a->groups * n_blk * 4);
-    a->list = take((size_t)a->chunks * a->tcap * a->groups * a->tq * 4);
-    a->tiles = take((size_t)a->chunks * a->tcap * a->groups * sizeof(BlockTile));
+    const size_t ord = (size_t)entries * a->groups * 4, cnt = (size_t)a->groups * n_blk * 4;   // of a chunk
+    const size_t list = (size_t)a->tcap * a->groups * a->tq * 4, tiles = (size_t)a->tcap * a->groups * sizeof(BlockTile);
+    const size_t ml = (size_t)entries * s->H * a->objs * 8;
+    const int64_t most = std::max<int64_t>(1, (int64_t)(LISTS_MOST / (ord + cnt * (1 + a->runs) + list + tiles + ml)));
+    const int64_t sections = (a->chunks + most - 1) / most;   // (several chunks are those of one object)
+    a->chunks = (int)((a->chunks + sections - 1) / sections);
+    a->section = (int64_t)a->chunk * a->chunks;
+    a->ord = take(ord * a->chunks);
+    a->cnt = take(cnt * a->chunks);
+    a->base = take(cnt * a->chunks * a->runs);
+    a->list = take(list * a->chunks);
+    a->tiles = take(tiles * a->chunks);
     a->opart = take(entries * s->H * a->objs * s->d_h * elem(s->dt));
-    a->ml = take((size_t)s->n_q * slots * s->H * a->objs * 8);
+    a->ml = take(ml * a->chunks);
   } else {
     // a work-group per CU, each with a few pieces of 32 keys per wave (whole rows and
     // splits in us, 8 key heads of 128: one row of 64 of 2048 blocks 31/14, four rows
@@ -402,32 +413,34 @@ rs3_status rs3_block_attend(const rs3_block_shape* s, const void* Q, const void*
   t.list = (uint32_t*)(w + pl.list);
   t.tiles = (BlockTile*)(w + pl.tiles);
   t.chunk = pl.chunk;
-  t.chunks = pl.chunks;
   t.run = pl.run;
   t.runs = pl.runs;
   t.tq = pl.tq;
   t.tcap = pl.tcap;
   part.S = a.slots;
   hipError_t e = hipSuccess;
-  for (int64_t o = 0; o < s->n_obj && e == hipSuccess; o += pl.objs) {
-    const int64_t es = (int64_t)elem(s->dt), rows = o * s->n_q, lists = rows * s->H_kv;
-    a.n_obj = (int)std::min<int64_t>(pl.objs, s->n_obj - o);
-    t.groups = a.n_obj * s->H_kv;
-    a.Q = (const uint8_t*)Q + o * s->q_obj_stride * es;
-    a.K = (const uint8_t*)K + o * s->k_obj_stride * es;
-    a.V = (const uint8_t*)V + o * s->v_obj_stride * es;
-    a.O = (uint8_t*)O + o * s->o_obj_stride * es;
-    a.idx = idx + lists * s->top_k;
-    a.count = count + lists;
-    a.n_vis = n_vis ? n_vis + rows : nullptr;
-    e = rs3_launch_block_lists(a, t, part, st);
-    for (t.ch = 0; t.ch < pl.chunks && e == hipSuccess; ++t.ch) {
-      part.i0 = t.ch * pl.chunk;
-      part.nq = t.nq = std::min(pl.chunk, s->n_q - part.i0);
-      e = rs3_launch_block_tile(a, t, part, s->dt, st);
-      if (e == hipSuccess) e = rs3_launch_block_merge(a, part, s->dt, true, st);
+  for (int64_t o = 0; o < s->n_obj; o += pl.objs)
+    for (int64_t q = 0; q < s->n_q && e == hipSuccess; q += pl.section) {
+      const int64_t es = (int64_t)elem(s->dt), rows = o * s->n_q + q, lists = rows * s->H_kv;
+      a.n_obj = (int)std::min<int64_t>(pl.objs, s->n_obj - o);
+      a.n_q = (int)std::min<int64_t>(pl.section, s->n_q - q);   // all of them where there are several objects
+      t.groups = a.n_obj * s->H_kv;
+      t.chunks = (a.n_q + pl.chunk - 1) / pl.chunk;
+      a.Q = (const uint8_t*)Q + (o * s->q_obj_stride + q * s->q_stride) * es;
+      a.K = (const uint8_t*)K + o * s->k_obj_stride * es;
+      a.V = (const uint8_t*)V + o * s->v_obj_stride * es;
+      a.O = (uint8_t*)O + (o * s->o_obj_stride + q * s->o_stride) * es;
+      a.idx = idx + lists * s->top_k;
+      a.count = count + lists;
+      a.n_vis = n_vis ? n_vis + rows : nullptr;
+      e = rs3_launch_block_lists(a, t, part, st);
+      for (t.ch = 0; t.ch < t.chunks && e == hipSuccess; ++t.ch) {
+        part.i0 = t.ch * pl.chunk;
+        part.nq = t.nq = std::min(pl.chunk, a.n_q - part.i0);
+        e = rs3_launch_block_tile(a, t, part, s->dt, st);
+        if (e == hipSuccess) e = rs3_launch_block_merge(a, part, s->dt, true, st);
+      }
     }
-  }
   return map_err(e);
 }
 

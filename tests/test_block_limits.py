@@ -69,3 +69,29 @@ def test_select_workspace_does_not_grow_with_the_queries(p):
     assert select_bytes(p, 0, 1 << 26, 8, 8, 128, 32, 16) == 0
     # as long as they fit, the scores of all rows
     assert select_bytes(p, 1, 1 << 20, 8, 8, 128, 64, 16) == 8 * (1 << 14) * 8
+
+
+def attend_bytes(p, n_q, n_kv, H, H_kv, d_h, block, top_k, n_obj=1, dt=1):
+    return p.block_attend_workspace_size(p.block_shape(p.RS3_BF16 if dt else p.RS3_F32, n_obj, n_q, n_kv, H, H_kv, d_h, block,
+                                                       top_k))
+
+
+def test_attend_workspace_does_not_grow_with_the_queries(p):
+    """1 GiB of partial rows, and lists and (m, l) pairs of 256 MiB; or those of one
+    chunk of queries, whose lists have a few queries' places per block of the
+    keys (an eighth of the bytes of their keys and values)."""
+    rng = np.random.default_rng(4)
+    cases = [(131072, 131072, 32, 8, 128, 64, 64), (1 << 22, 262144, 256, 256, 32, 32, 255), (1 << 22, 8192, 8, 8, 32, 32, 256),
+             (65536, 131072, 32, 8, 128, 64, 64), (1024, 262144, 8, 8, 64, 32, 100, 4096), (300000, 5000, 40, 8, 64, 64, 17, 2, 0)]
+    for _ in range(3000):
+        H_kv = int(rng.choice([1, 2, 4, 8, 32, 256]))
+        H = H_kv * int(rng.choice([1, 3, 8]))
+        n_obj = int(rng.choice([1, 1, 3, 64, 4096]))
+        n_q = int(2 ** rng.uniform(3, 22)) // n_obj
+        if H <= 256 and n_q:
+            cases.append((n_q, int(2 ** rng.uniform(4, 24)), H, H_kv, int(rng.choice([32, 64, 128, 256])),
+                          int(rng.choice([32, 64, 128, 256])), int(2 ** rng.uniform(0, 8)), n_obj, int(rng.integers(0, 2))))
+    for c in cases:
+        n_kv, H_kv, d_h, n_obj = c[1], c[3], c[4], c[7] if len(c) > 7 else 1
+        keys = 2 * n_obj * H_kv * n_kv * d_h * (2 if len(c) < 9 or c[8] else 4)
+        assert attend_bytes(p, *c) <= (1 << 30) + max(256 << 20, (320 << 20) + keys // 8), c

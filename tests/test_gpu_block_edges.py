@@ -198,3 +198,35 @@ def test_block_select_of_more_rows_than_the_scores_workspace_holds(dtype):
         ei, ec = B.block_select(storage_to_f64(Q[o:o + 1, i:i + 1], dtype), storage_to_f64(M[o:o + 1], dtype),
                                 v[o:o + 1, i:i + 1], block, top_k, 1, 2, n_kv)
         assert np.array_equal(idx[o, i], ei[0, 0]) and np.array_equal(count[o, i], ec[0, 0])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_block_attend_of_more_queries_than_the_lists_workspace_holds(dtype):
+    """1,200,001 queries, whose lists are made in parts: the same bits as for a part
+    of the queries in a call of its own, and at the parts' border the oracle's."""
+    p = rs3()
+    n_q, n_kv, H, H_kv, d_h, block, top_k = 1200001, 500, 4, 4, 32, 32, 8
+    gen = torch.Generator(device="cuda").manual_seed(6)
+    dt, nb = (torch.bfloat16 if dtype == "bf16" else torch.float32), -(-n_kv // block)
+    Q = torch.randn((1, n_q, H, d_h), generator=gen, device="cuda", dtype=dt)
+    K, V = (torch.randn((1, n_kv, H_kv, d_h), generator=gen, device="cuda", dtype=dt) for _ in range(2))
+    idx = torch.rand((1, n_q, H_kv, nb), generator=gen, device="cuda").argsort(-1)[..., :top_k].sort(-1).values.int()
+    count = torch.randint(0, top_k + 1, (1, n_q, H_kv), generator=gen, device="cuda", dtype=torch.int32)
+    v = torch.randint(0, n_kv + 1, (1, n_q), generator=gen, device="cuda", dtype=torch.int32)
+
+    def run(a, b):
+        s = p.block_shape(dt_of(dtype), 1, b - a, n_kv, H, H_kv, d_h, block, top_k)
+        O = torch.full((1, b - a, H, d_h), float("nan"), dtype=dt, device="cuda")
+        ws = torch.full((p.block_attend_workspace_size(s),), 0xFF, dtype=torch.uint8, device="cuda")
+        p.block_attend(s, Q[:, a:b], K, V, idx[:, a:b], count[:, a:b], O, n_vis=v[:, a:b], ws=ws)
+        torch.cuda.synchronize()
+        return O, ws.numel()
+    O, size = run(0, n_q)
+    assert size < (1 << 30) + n_q * top_k * H * 16        # not the lists and pairs of all queries
+    for a in range(0, n_q, 150001):   # each of them many queries too
+        b = min(a + 150001, n_q)
+        assert torch.equal(O[:, a:b], run(a, b)[0]), a
+    at = np.unique(np.clip(np.concatenate([np.arange(-3, 4) + k * n_q // 12 for k in range(13)]), 0, n_q - 1))
+    f = lambda t: host(t.contiguous(), dtype)  # noqa: E731
+    check_attend(f(O[:, at]), f(Q[:, at]), f(K), f(V), idx[:, at].cpu().numpy(), count[:, at].cpu().numpy(),
+                 v[:, at].cpu().numpy(), block, dtype)
