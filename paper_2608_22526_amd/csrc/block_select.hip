@@ -736,10 +736,10 @@ __global__ __launch_bounds__(64 * NWS, 4) void k_select_tile(BlockSelectArgs p, 
       if (lane == 0) p.count[row] = n + rr.nb - rr.last0;
     };
     // scores from w_hi on are kept, and `need` of the `cand` ones from w_lo to below it
-    // (none where the forced blocks fill the list, whatever the scores)
+    // (where the forced blocks fill the list, none: no score compares with NaN)
     bool is_hard = false;
     int cand = 0, need = 0;
-    float w_lo = INFINITY, w_hi = INFINITY;
+    float w_lo = NAN, w_hi = NAN;
     if (rr.want > 0) {
       if (!(qn[r] * sqrtf(k2) < 1e38f)) {   // a score may leave the fp32 range, or is no number
         is_hard = true;
@@ -840,7 +840,7 @@ __global__ __launch_bounds__(64 * NWS, 4) void k_select_tile(BlockSelectArgs p, 
     }
     int out = 0, c = 0;
     auto emit = [&](int j, float v) {
-      uint64_t m = __ballot(rr.want > 0 && v >= w_hi) | forced_bits(rr, j);
+      uint64_t m = __ballot(v >= w_hi) | forced_bits(rr, j);
       if (cand > 0) {
         const bool in = v >= w_lo && v < w_hi;
         const uint64_t im = __ballot(in);
