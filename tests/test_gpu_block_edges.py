@@ -230,3 +230,73 @@ def test_block_attend_of_more_queries_than_the_lists_workspace_holds(dtype):
     f = lambda t: host(t.contiguous(), dtype)  # noqa: E731
     check_attend(f(O[:, at]), f(Q[:, at]), f(K), f(V), idx[:, at].cpu().numpy(), count[:, at].cpu().numpy(),
                  v[:, at].cpu().numpy(), block, dtype)
+
+
+# ---- layouts -----------------------------------------------------------------------
+@pytest.mark.parametrize("n_q", [1, 2000])
+def test_keys_and_values_past_32_bit_offsets(n_q):
+    """Rows almost 2^22 elements apart (9 GB): the same bits as with packed rows."""
+    p = rs3()
+    n_kv, H, H_kv, d_h, block, top_k, row = 1100, 4, 2, 64, 32, 12, (1 << 22) - 8
+    gen = torch.Generator(device="cuda").manual_seed(n_q)
+    rand = lambda *shape: torch.randn(shape, generator=gen, device="cuda", dtype=torch.bfloat16)  # noqa: E731
+    Q, K, V = rand(1, n_q, H, d_h), rand(1, n_kv, H_kv, d_h), rand(1, n_kv, H_kv, d_h)
+    far = torch.empty((n_kv, row), dtype=torch.bfloat16, device="cuda")
+    at = row - 2 * H_kv * d_h
+    far[:, at:at + H_kv * d_h], far[:, at + H_kv * d_h:] = K.view(n_kv, -1), V.view(n_kv, -1)
+
+    def run(K, V, **strides):
+        s = p.block_shape(p.RS3_BF16, 1, n_q, n_kv, H, H_kv, d_h, block, top_k, 1, 1, **strides)
+        M = torch.full((1, H_kv, -(-n_kv // block), d_h), 9.0, dtype=torch.bfloat16, device="cuda")
+        idx = torch.full((1, n_q, H_kv, top_k), 77, dtype=torch.int32, device="cuda")
+        count, O = torch.full((1, n_q, H_kv), 77, dtype=torch.int32, device="cuda"), torch.full_like(Q, float("nan"))
+        ws = torch.empty(max(p.block_select_workspace_size(s), p.block_attend_workspace_size(s), 16), dtype=torch.uint8,
+                         device="cuda")
+        p.block_means(s, K, M)
+        p.block_select(s, Q, M, idx, count, ws=ws)
+        p.block_attend(s, Q, K, V, idx, count, O, ws=ws)
+        torch.cuda.synchronize()
+        return M, idx, count, O
+    packed = run(K, V)
+    assert torch.isfinite(packed[3]).all()
+    apart = run(far[:, at:], far[:, at + H_kv * d_h:], k_stride=row, v_stride=row, k_obj_stride=0, v_obj_stride=0)
+    for a, b in zip(packed, apart):
+        assert torch.equal(a, b)
+
+
+def test_two_streams_at_once():
+    """The same calls in flight on two streams, with outputs and workspaces of their
+    own, against one after the other."""
+    p = rs3()
+    n_obj, n_q, n_kv, H, H_kv, d_h, block, top_k = 2, 1500, 2000, 4, 2, 128, 64, 9
+    s = p.block_shape(p.RS3_BF16, n_obj, n_q, n_kv, H, H_kv, d_h, block, top_k, 1, 1)
+    gen = torch.Generator(device="cuda").manual_seed(8)
+    rand = lambda *shape: torch.randn(shape, generator=gen, device="cuda", dtype=torch.bfloat16)  # noqa: E731
+    sides = []
+    for _ in range(2):
+        Q, K, V = rand(n_obj, n_q, H, d_h), rand(n_obj, n_kv, H_kv, d_h), rand(n_obj, n_kv, H_kv, d_h)
+        need = max(p.block_select_workspace_size(s), p.block_attend_workspace_size(s), 16)
+        outs = lambda: (torch.zeros((n_obj, H_kv, -(-n_kv // block), d_h), dtype=torch.bfloat16, device="cuda"),  # noqa: E731
+                        torch.zeros((n_obj, n_q, H_kv, top_k), dtype=torch.int32, device="cuda"),
+                        torch.zeros((n_obj, n_q, H_kv), dtype=torch.int32, device="cuda"), torch.zeros_like(Q),
+                        torch.empty(need, dtype=torch.uint8, device="cuda"))
+        sides.append((Q, K, V, outs(), outs(), torch.cuda.Stream()))
+
+    def calls(Q, K, V, out):
+        M, idx, count, O, ws = out
+        p.block_means(s, K, M)
+        p.block_select(s, Q, M, idx, count, ws=ws)
+        p.block_attend(s, Q, K, V, idx, count, O, ws=ws)
+    for Q, K, V, one, _, _ in sides:
+        calls(Q, K, V, one)
+    torch.cuda.synchronize()
+    for _ in range(3):
+        for Q, K, V, _, two, st in sides:
+            with torch.cuda.stream(st):
+                for t in two[:4]:
+                    t.zero_()
+                calls(Q, K, V, two)
+    torch.cuda.synchronize()
+    for _, _, _, one, two, _ in sides:
+        for a, b in zip(one[:4], two[:4]):
+            assert torch.equal(a, b)
