@@ -457,8 +457,8 @@ def qk_norm_rope(n: int, Q, H: int, K, H_kv: int, d_h: int, dtype: int, Qo, Ko, 
                  ko_stride: Optional[int] = None, stream=None):
     """RMS norm of each head of Q [n][H][d_h] and K [n][H_kv][d_h] (None with
     0 heads) and the rotation of its first d_rot channels by table[pos]."""
-    if (n | H | H_kv | d_h | d_rot) >> 31:
-        _check_i32(n, H, H_kv, d_h, d_rot)
+    if (n | H | H_kv | d_h | d_rot | pairing) >> 31:
+        _check_i32(n, H, H_kv, d_h, d_rot, pairing)
     torch, dev, st = _call()
     dt, f32 = torch.bfloat16 if dtype == RS3_BF16 else torch.float32, torch.float32
     wq, wk = H * d_h, H_kv * d_h

@@ -95,3 +95,8 @@ def test_attend_workspace_does_not_grow_with_the_queries(p):
         n_kv, H_kv, d_h, n_obj = c[1], c[3], c[4], c[7] if len(c) > 7 else 1
         keys = 2 * n_obj * H_kv * n_kv * d_h * (2 if len(c) < 9 or c[8] else 4)
         assert attend_bytes(p, *c) <= (1 << 30) + max(256 << 20, (320 << 20) + keys // 8), c
+
+
+def test_binding_refuses_a_pairing_past_32_bits(p):
+    with pytest.raises(ValueError):
+        p.qk_norm_rope(1, None, 0, None, 0, 64, p.RS3_BF16, None, None, pairing=2 ** 32 + 1)
