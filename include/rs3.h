@@ -418,7 +418,8 @@ rs3_status rs3_attend(const void* Qh, const void* Kh, const void* Vh, int32_t n_
  * rs3_block_attend): every head x of a row becomes
  *   y = x / sqrt(mean_c(x_c^2) + eps) * gain
  * and then its first d_rot channels are turned in pairs by the factors of the
- * row's position, both in fp32, rounded to `dt` once.  Pair p of a head takes
+ * row's position, both in fp32, rounded to `dt` once (a head whose squares leave
+ * the fp32 range becomes 0).  Pair p of a head takes
  * column p of the table: channels (2p, 2p+1) with RS3_PAIRS_ADJACENT (as the
  * layers' tables, see rs3_layer_set_rope) or (p, p + d_rot/2) with
  * RS3_PAIRS_HALVES; (a, b) becomes (a cos - b sin, a sin + b cos).
@@ -456,7 +457,8 @@ rs3_status rs3_qk_norm_rope(int32_t n, const void* Q, int64_t q_stride, int32_t 
  *   rs3_block_attend : softmax attention over the keys of those blocks.
  * The shape and the row layouts are shared by the three:
  * n_obj   : caches (objects, streams), 1 .. 4096
- * n_q     : query rows per object (0: nothing is done); n_obj*n_q <= 2^22
+ * n_q     : query rows per object (0: nothing is done; rs3_block_means does not
+ *           use it); n_obj*n_q <= 2^22
  * n_kv    : key rows per object, at most 2^26 (0: no keys)
  * H, H_kv : query heads and key heads, H a multiple of H_kv, H <= 256; query
  *           head h reads key head h / (H / H_kv)
@@ -490,8 +492,8 @@ typedef struct {
   int64_t q_stride, q_obj_stride, k_stride, k_obj_stride, v_stride, v_obj_stride, o_stride, o_obj_stride;
 } rs3_block_shape;
 
-/* Kmean [n_obj][H_kv][n_blk][d_h]: the mean of the keys of each block, summed
- * in fp64 and rounded to `dt` once.
+/* Kmean [n_obj][H_kv][n_blk][d_h]: the mean of the keys of each block, in fp64
+ * and rounded to `dt` once.
  * kv_len : device int32 [n_obj], the keys that each object has so far (taken
  *          into [0, n_kv]), NULL for n_kv: the mean of a block is that of its
  *          keys below kv_len.
@@ -523,8 +525,18 @@ rs3_status rs3_block_select(const rs3_block_shape* s /*[host]*/, const void* Q, 
  * them, or the caller's own lists: a count is taken into [0, min(top_k,
  * n_blk)], and an entry that is out of range or not above the entry before it
  * takes no part.
- * Logits of -inf have weight 0.  The bf16 form rounds the weights to bf16 for
- * the matrix cores; sums are fp32, and O is rounded to `dt` once.
+ * Logits of -inf have weight 0, as have those whose weight is below the fp32
+ * range; 0 times an infinite value is no number, unless all weights of the keys
+ * that are computed together are 0.
+ * In bf16 the weights are rounded to bf16 for the matrix cores (2^-8 of a weight,
+ * and their sum is that of the rounded ones), and for many queries the partial
+ * row of every listed block to f16 times a power of two (2^-11 of each value down
+ * to 2^-28 of the row's largest) before the partials are joined; sums are fp32,
+ * and O is rounded to bf16 last.  In fp32 everything is fp32.  Which of the two
+ * forms runs goes by the sizes alone, so that a row may differ within these bounds
+ * with the number of queries beside it.
+ * Many queries share the reads of a block up to 8,192 blocks; past those every
+ * query reads its blocks for itself.
  * ws : at least rs3_block_attend_workspace_size() bytes: for many queries up to
  *      1 GiB of partial rows, those of a chunk of the queries at a time, and 256 MiB
  *      of lists and (m, l) pairs, or those of one chunk (an eighth of K and V and

@@ -38,10 +38,12 @@ struct RowLayout {
 // piece ahead, so that no barrier stands between the pieces.  The G query heads
 // of the key head are the columns of 16x16 products: S^T = K Q^T, and the
 // weights feed O^T += V^T P^T from their registers.  Keys past the last that
-// the query sees read that one again; their weights and values are 0.  In bf16 the weights are rounded
-// for the products (2^-8 of a weight, as O's own rounding), and their sum is of the
-// rounded ones.  Bound by the read of the keys and values: one token of 32 streams,
-// 32 heads of 128 to 8, 2048 of up to 16384 keys each, 269 MB in 50 us (5.4 TB/s).
+// the query sees read that one again; their weights and values are 0.  In bf16 the
+// weights are rounded for the products (2^-8 of a weight, as O's own rounding), and
+// their sum is of the rounded ones.  Bound by the read of the keys and values: one
+// token of 32 streams, 32 heads of 128 to 8, 2048 of up to 16384 keys each, 269 MB in
+// 50 us (5.4 TB/s), in fp32 538 MB in 95 (5.7).  Few waves (fp32 heads of 256: two, 8
+// query heads to 2 key heads, 1024 keys of 32 streams) 135 MB in 39 us (3.5).
 template <class T, int D, int NW>
 __global__ __launch_bounds__(64 * NW) void k_block_row(BlockAttendArgs p, BlockPartArgs part, int HT) {
   using L = RowLayout<T, D>;

@@ -7,7 +7,8 @@
 //  k_select_row  : a work-group per (query, key head), every score in fp64.  For
 //      few queries, where the read of the mean keys is the bound and the fp64
 //      units have time: one token of 32 streams, up to 2048 blocks of 8 key heads of
-//      128, 81 MB in 25 us (3.2 TB/s).
+//      128, 81 MB in 25 us (3.2 TB/s); streams of 2048 blocks each, 134 MB in 34
+//      (4.0): a row per CU, the longest of which ends last.
 //  k_select_tile : up to 32 queries of a key head per work-group, scores on the
 //      bf16 matrix cores with a bound on their error.  A row whose top_k-th score
 //      stands clear of the next by twice the bound is done; otherwise the blocks
@@ -15,7 +16,9 @@
 //      hundred, two or three blocks each), and where there are many of them (equal
 //      keys, zero queries, values that are no numbers) the whole row is.  4096 prompt
 //      tokens, 4 key heads of 128 and up to 512 blocks in 30 us: scores 14, the rest
-//      the choice, which is bound by instruction issue.
+//      the choice.  Bound by each wave's chain of dependent steps: two work-groups
+//      per CU are all there is, vector instructions take 57 % of the SIMDs' cycles, and
+//      of the waves' time 45 % waits for data or barriers, 22 % for an issue slot.
 #include "block.h"
 
 namespace rs3 {
